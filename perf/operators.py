@@ -143,7 +143,7 @@ def prepare(case, seed):
         s["y"], s["r"] = randn(T, d, dtype=dt, scale=0.3), randn(T, d, dtype=rt)
         s["w_post"] = (1 + randn(d, scale=0.1)) if case["post"] else None
         s["w_pre"] = 1 + randn(d, scale=0.1)
-        s["gate"] = {"none": None, "channel": randn(d, scale=0.5), "token": torch.sigmoid(randn(T))}[case["gate"]]
+        s["gate"] = {"none": None, "channel": randn(d, scale=0.5), "token": torch.sigmoid(randn(T, 1))}[case["gate"]]
         if case["op"] == "norm_grad":
             # the loss's gradients of the normed output and of the stream, and what the forward kept of its rows
             s["d_n"], s["d_r_out"] = randn(T, d, dtype=torch.bfloat16), randn(T, d, dtype=rt)
@@ -182,7 +182,7 @@ def _norm_plain(s):
         s_y = torch.rsqrt((z * z).mean(1, keepdim=True) + _EPS)
         z = z * s_y * s["w_post"]
     if s["gate"] is not None:
-        z = z * (s["gate"] if s["case"]["gate"] == "channel" else s["gate"][:, None])
+        z = z * s["gate"]
     r_out = _RES_SCALE * s["r"].float() + _BLOCK_SCALE * z
     s_r = torch.rsqrt((r_out * r_out).mean(1, keepdim=True) + _EPS)
     return r_out, r_out * s_r * s["w_pre"], torch.cat([s_y, s_r], 1)
@@ -193,7 +193,7 @@ def _norm_grad_plain(s):
     s_y, s_r = s["stats"][:, :1], s["stats"][:, 1:]
     yn = y * s_y
     z = yn * s["w_post"] if c["post"] else yn
-    gate = {"none": 1.0, "channel": s["gate"], "token": s["gate"][:, None] if c["gate"] == "token" else None}[c["gate"]]
+    gate = 1.0 if s["gate"] is None else s["gate"]
     r_out = _RES_SCALE * s["r"].float() + _BLOCK_SCALE * gate * z
     rn = r_out * s_r
     u = d_n * s["w_pre"]
@@ -207,7 +207,8 @@ def _norm_grad_plain(s):
     else:
         out["d_y"] = dz.to(s["y"].dtype)
     if c["gate"] != "none":
-        out["d_gate"] = (_BLOCK_SCALE * z * G).sum(0 if c["gate"] == "channel" else 1)
+        terms = _BLOCK_SCALE * z * G
+        out["d_gate"] = terms.sum(0) if c["gate"] == "channel" else terms.sum(1, keepdim=True)
     return out
 
 
@@ -319,7 +320,7 @@ def exact(case, seed):
 
         z = rms(v["y"], v["w_post"]) if case["post"] else v["y"]
         if case["gate"] != "none":
-            z = z * (v["gate"] if case["gate"] == "channel" else v["gate"].unsqueeze(1))
+            z = z * v["gate"]
         r_out = v["r"] * _RES_SCALE + z * _BLOCK_SCALE
         n = rms(r_out, v["w_pre"])
         if op == "norm":
