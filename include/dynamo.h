@@ -382,6 +382,87 @@ dynamo_status dynamo_route_permute_static(const float* router_logits, int32_t T,
                                           int32_t renormalize, int32_t* topk_idx, float* topk_w,
                                           int32_t* expert_offsets, int32_t* perm, void* stream);
 
+/* ---- Operators around the layer --------------------------------------------------------------------------------------
+ * What a decoder block needs next to dynamo_moe_forward.  They take no context: device buffers, sizes and a stream, which
+ * has to belong to the current device.  Every call is asynchronous and stream-ordered, can be captured in a CUDA graph, keeps
+ * nothing between calls and gives the same bits for the same inputs (no floating-point atomics).  Row-major contiguous
+ * arrays, 16-byte aligned (ERR_ALIGN); a *_dtype is DYNAMO_BF16 or DYNAMO_F32 (ERR_SHAPE otherwise); widths are multiples of
+ * 8 (ERR_SHAPE).  Outputs must not overlap inputs or one another unless stated.  Sums, norms and weights are worked out in
+ * fp32, results rounded once.  T = 0 is a no-op unless stated.
+ *
+ * Tokens sorted by expert and back (Section II-A: one-to-many dispatch; for experts other than the layer's own, and for
+ * training what stands around them).
+ * dynamo_dispatch: stable counting sort of the (token, slot) pairs by expert, and each token's row copied to its places.
+ *   topk_idx       : int32 [T, k]; a value outside [0, n_experts) drops the pair (it goes to no expert)
+ *   x, rows        : [T, d] and up to T * k rows of d, of type dtype; both NULL: sort alone (d and dtype are not read)
+ *   expert_offsets : int32 [n_experts + 1] first row of every expert, the number of kept pairs at the end (also for T = 0)
+ *   perm           : int32 [T * k] row -> t * k + j;  pos : int32 [T, k] pair -> row, -1 for a dropped one
+ *   Entries of perm and rows behind the last kept pair stay as they were.
+ *   workspace      : dynamo_dispatch_workspace_bytes (0 for small T * k: then it may be NULL), 256-byte aligned
+ *   1 <= n_experts <= 256, 1 <= top_k <= min(8, n_experts) (ERR_SHAPE), T * top_k < 2^31 (ERR_TOKENS).
+ * dynamo_combine: y[t] = sum_j topk_w[t,j] * rows[pos[t,j]], in the order of j; a token without a kept pair gives zeros.
+ *   topk_w fp32 [T, k], not used where pos is negative; NULL: ones, which makes the call the gradient of dynamo_dispatch
+ *   (dx from the rows' gradients).  rows has T * k rows as far as pos names them; a pos outside [0, T * k) counts as dropped.
+ * dynamo_combine_backward: the gradient of dynamo_combine.  From dy [T, d] of type dy_dtype:
+ *   d_rows[pos[t,j]] = topk_w[t,j] * dy[t] (rows' type; other rows stay as they were) and, unless d_w is NULL,
+ *   d_w[t,j] = <rows[pos[t,j]], dy[t]> (fp32; 0 for dropped pairs).  No two pairs may share a row. */
+dynamo_status dynamo_dispatch_workspace_bytes(int32_t T, int32_t n_experts, int32_t top_k, size_t* bytes);
+dynamo_status dynamo_dispatch(const int32_t* topk_idx, int32_t T, int32_t n_experts, int32_t top_k, const void* x, int32_t d,
+                              int32_t dtype, int32_t* expert_offsets, int32_t* perm, int32_t* pos, void* rows,
+                              void* workspace, size_t workspace_bytes, void* stream);
+dynamo_status dynamo_combine(const void* rows, int32_t dtype, const int32_t* pos, const float* topk_w, int32_t T,
+                             int32_t top_k, int32_t d, void* y, int32_t y_dtype, void* stream);
+dynamo_status dynamo_combine_backward(const void* dy, int32_t dy_dtype, const void* rows, int32_t dtype, const int32_t* pos,
+                                      const float* topk_w, int32_t T, int32_t top_k, int32_t d, void* d_rows, float* d_w,
+                                      void* stream);
+
+/* Where a block's output joins the residual stream: the norm behind the block, its gate and the residual scale, and the
+ * norm in front of the next block, in one pass.
+ *   z = y * rsqrt(mean(y^2) + eps) * w_post  (post_norm; else z = y),   r_out = res_scale * r + block_scale * gate * z,
+ *   n_out = r_out * rsqrt(mean(r_out^2) + eps) * w_pre  (pre_norm; of r_out before it is rounded to its type)
+ *   y     : [T, d] y_dtype, the block's output; NULL: r_out is r itself (nothing is stored, post_norm, gate and the scales are
+ *           not used), which leaves the norm in front of a block
+ *   r, r_out : [T, d] r_dtype; r_out may be r.   n_out : [T, d] n_dtype
+ *   w_post, w_pre : [d] w_dtype or NULL (ones).   gate : [d] w_dtype (GATE_CHANNEL), [T] fp32 (GATE_TOKEN) or none
+ *   stats : fp32 [T, 2] or NULL: the two rsqrt factors of every row (1 where there is no norm), which the gradient reads
+ * dynamo_norm_join_backward: from d_n (gradient of n_out, n_dtype; not read without pre_norm) and d_r_out (of r_out, r_dtype;
+ *   NULL: zero, allowed with pre_norm only), and r, y, stats, weights and gate as the forward had them.  Each output may be
+ *   NULL: d_r [T, d] r_dtype, d_y [T, d] y_dtype, fp32 d_w_post [d], d_w_pre [d], d_gate ([d] or [T]).  Sums over the tokens are in a
+ *   fixed order.  workspace: dynamo_norm_join_workspace_bytes, 256-byte aligned, needed for gradients of weights and of a channel
+ *   gate.  T = 0 sets these to zero.
+ * d <= 16384 (ERR_SHAPE); eps > 0, scales finite, gate_kind in the list, no gradient asked of what is not there, y or
+ * pre_norm (ERR_ARG). */
+enum { DYNAMO_GATE_NONE = 0, DYNAMO_GATE_CHANNEL = 1, DYNAMO_GATE_TOKEN = 2 };
+typedef struct {
+    int32_t d;
+    int32_t y_dtype, r_dtype, n_dtype, w_dtype;
+    int32_t gate_kind;
+    int32_t post_norm, pre_norm;
+    float res_scale, block_scale, eps;
+} dynamo_join_desc;
+dynamo_status dynamo_norm_join_forward(const dynamo_join_desc* desc, const void* r, const void* y, const void* w_post,
+                                       const void* gate, const void* w_pre, int32_t T, void* r_out, void* n_out,
+                                       float* stats, void* stream);
+dynamo_status dynamo_norm_join_workspace_bytes(const dynamo_join_desc* desc, int32_t T, size_t* bytes);
+dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void* d_n, const void* d_r_out, const void* r,
+                                        const void* y, const float* stats, const void* w_post, const void* gate,
+                                        const void* w_pre, int32_t T, void* d_r, void* d_y, float* d_w_post, float* d_gate,
+                                        float* d_w_pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Products with a 4-bit matrix that has group scales: the block's other projections, in the experts' quantizer.
+ * dynamo_linear_quantize: w bf16 [rows, cols] -> codes uint8 [rows, cols / 2] (index 2i in the low, 2i + 1 in the high half of
+ *   byte i) and params fp16 [rows, cols / G, 2] {scale, zero}, by the rule of dynamo_pack_experts at 4 bits.
+ * dynamo_linear_forward: y[t][n] = sum_k (scale[n][k/G] * code[n][k] + zero[n][k/G]) * x[t][k]
+ *   x bf16 [T, cols], y [T, rows] of y_dtype.  Products are exact, sums in fp32.  Made for the few rows of a decode step; the
+ *   matrix is read once per 32 tokens at most.  An infinite or NaN activation makes its row NaN; the sum of 31 |x| over a group
+ *   has to stay in the range of fp32.
+ * group_size 64 or 128, cols a multiple of it, rows >= 1 (ERR_SHAPE); 0 <= T <= DYNAMO_LINEAR_MAX_TOKENS (ERR_TOKENS). */
+#define DYNAMO_LINEAR_MAX_TOKENS 65536
+dynamo_status dynamo_linear_quantize(const void* w, int32_t rows, int32_t cols, int32_t group_size, void* codes, void* params,
+                                     void* stream);
+dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size,
+                                    const void* codes, const void* params, void* y, int32_t y_dtype, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,8 @@ MAT_GATE, MAT_UP, MAT_DOWN = 0, 1, 2
 OPERAND_FP16, OPERAND_BF16 = 0, 1
 CODES_BASE, CODES_HI_POOL, CODES_HI_ACTIVE = 0, 1, 2
 SWITCH_SELECT, SWITCH_REQUANT = 0, 1
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
+LINEAR_MAX_TOKENS = 65536
 
 STATUS_NAMES = ["OK", "ERR_NULL", "ERR_SHAPE", "ERR_BITS", "ERR_ALIGN", "ERR_ARENA_TOO_SMALL", "ERR_INDEX_RANGE",
                 "ERR_INDEX_DUP", "ERR_NOT_CACHED", "ERR_STATE", "ERR_TOKENS", "ERR_CUDA", "ERR_TIMEOUT", "ERR_ARG", "ERR_RANGE"]
@@ -37,6 +39,9 @@ EXPORTED = ["dynamo_create", "dynamo_destroy", "dynamo_arena_bytes", "dynamo_pac
             "dynamo_set_channel_precision_down",
             "dynamo_get_channel_stats", "dynamo_select_significant", "dynamo_sync_sets", "dynamo_route_permute_static",
             "dynamo_debug_expire_wait", "dynamo_debug_check_guards",
+            "dynamo_dispatch_workspace_bytes", "dynamo_dispatch", "dynamo_combine", "dynamo_combine_backward",
+            "dynamo_norm_join_forward", "dynamo_norm_join_workspace_bytes", "dynamo_norm_join_backward",
+            "dynamo_linear_quantize", "dynamo_linear_forward",
             "dynamo_kernel_launches", "dynamo_status_str"]
 
 
@@ -49,6 +54,12 @@ class LayerDesc(ctypes.Structure):
 class DebugOut(ctypes.Structure):
     _fields_ = [("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p), ("expert_offsets", ctypes.c_void_p),
                 ("perm", ctypes.c_void_p)]
+
+
+class JoinDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("d", "y_dtype", "r_dtype", "n_dtype", "w_dtype", "gate_kind", "post_norm",
+                                               "pre_norm")] +
+                [(n, ctypes.c_float) for n in ("res_scale", "block_scale", "eps")])
 
 
 class DynamoError(RuntimeError):
@@ -98,6 +109,16 @@ def load():
         L.dynamo_route_permute_static.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
         L.dynamo_debug_expire_wait.argtypes = [vp, ctypes.c_int64, vp]
         L.dynamo_debug_check_guards.argtypes = [vp, ctypes.POINTER(ctypes.c_int64), vp]
+        jd = ctypes.POINTER(JoinDesc)
+        L.dynamo_dispatch_workspace_bytes.argtypes = [i32, i32, i32, ctypes.POINTER(sz)]
+        L.dynamo_dispatch.argtypes = [vp, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.dynamo_combine.argtypes = [vp, i32, vp, vp, i32, i32, i32, vp, i32, vp]
+        L.dynamo_combine_backward.argtypes = [vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp]
+        L.dynamo_norm_join_forward.argtypes = [jd, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+        L.dynamo_norm_join_workspace_bytes.argtypes = [jd, i32, ctypes.POINTER(sz)]
+        L.dynamo_norm_join_backward.argtypes = [jd, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.dynamo_linear_quantize.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+        L.dynamo_linear_forward.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp]
         L.dynamo_kernel_launches.argtypes = [vp]
         L.dynamo_kernel_launches.restype = ctypes.c_int64
         L.dynamo_status_str.argtypes = [i32]

@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libdynamo.so")
 SOURCES = ["api.cu", "pack.cu", "route.cu", "switch.cu", "stats.cu", "ffn_stream.cu", "ffn_tc2.cu", "ffn_fold.cu",
-           "noalloc.cu", "assign.cu", "downside.cu", "debug.cu"]
+           "noalloc.cu", "assign.cu", "downside.cu", "debug.cu", "dispatch.cu", "norm_join.cu", "linear.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 CFLAGS = ARCH + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 LFLAGS = ARCH + ["-shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
