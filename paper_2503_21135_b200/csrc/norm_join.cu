@@ -58,183 +58,245 @@ __device__ __forceinline__ void weights8(const void* w, int w_f32, int c, float 
     }
 }
 
-// Sums of N values over the TPR threads of a row; every thread gets them.  `scratch`: [N][TPR / 32], two of them in turn.
-template <int TPR, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float* scratch) {
-    constexpr int W = TPR / 32;
+// Two fp32 values that one instruction works on (each rounded as by itself).
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ F2 f2(float both) { return f2(both, both); }
+__device__ __forceinline__ float lo(F2 a) { return __uint_as_float((uint32_t)a.v); }
+__device__ __forceinline__ float hi(F2 a) { return __uint_as_float((uint32_t)(a.v >> 32)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16>& r, F2 (&v)[4]) {
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if constexpr (W > 1) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) scratch[i * W + warp] = v[i];
-        __syncthreads();
-        // the warps' sums by 16-byte reads that all lanes share, added in the order of a tree
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float4 s = *reinterpret_cast<const float4*>(scratch + i * W);
-#pragma unroll
-            for (int w = 4; w < W; w += 4) {
-                const float4 q = *reinterpret_cast<const float4*>(scratch + i * W + w);
-                s.x += q.x, s.y += q.y, s.z += q.z, s.w += q.w;
-            }
-            v[i] = (s.x + s.y) + (s.z + s.w);
-        }
-    }
+    for (int i = 0; i < 4; ++i) v[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, F2 (&v)[4]) {
+    v[0] = f2(__uint_as_float(r.a.x), __uint_as_float(r.a.y));
+    v[1] = f2(__uint_as_float(r.a.z), __uint_as_float(r.a.w));
+    v[2] = f2(__uint_as_float(r.b.x), __uint_as_float(r.b.y));
+    v[3] = f2(__uint_as_float(r.b.z), __uint_as_float(r.b.w));
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const F2 (&v)[4]) {
+    const float f[8] = {lo(v[0]), hi(v[0]), lo(v[1]), hi(v[1]), lo(v[2]), hi(v[2]), lo(v[3]), hi(v[3])};
+    store8(p, f);
 }
 
+// Sum of a value over the TPR threads of a row; every thread gets it.  `scratch`: [TPR / 32], two of them in turn.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* scratch) {
+    constexpr int W = TPR / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (W > 1) {
+        if (lane == 0) scratch[warp] = v;
+        __syncthreads();
+        v = scratch[lane & (W - 1)];
+#pragma unroll
+        for (int o = W / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    }
+    return v;
+}
+// Sums of three values.  They are reduced together: at the first two steps a lane gives half of what it holds away and keeps
+// half, so that eight lanes end up with one of them each (6 shuffles instead of 15, and 3 instead of 12 across the warps).
+// `scratch`: [4][TPR / 32].
+template <int TPR>
+__device__ __forceinline__ void row_sums(float (&v)[3], float* scratch) {
+    constexpr int W = TPR / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool up16 = lane & 16, up8 = lane & 8;
+    const float k0 = (up16 ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up16 ? v[0] : v[2], 16);
+    const float k1 = (up16 ? 0.f : v[1]) + __shfl_xor_sync(0xffffffffu, up16 ? v[1] : 0.f, 16);
+    float k = (up8 ? k1 : k0) + __shfl_xor_sync(0xffffffffu, up8 ? k0 : k1, 8);   // value lane >> 3 (the fourth: nothing)
+#pragma unroll
+    for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
+    if constexpr (W > 1) {
+        constexpr int PER = W < 8 ? 1 : W / 8;
+        if ((lane & 7) == 0) scratch[(lane >> 3) * W + warp] = k;
+        __syncthreads();
+        const float* at = scratch + (lane >> 3) * W + (lane & (W / PER - 1) & 7) * PER;
+        k = at[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) k += at[i];
+#pragma unroll
+        for (int o = W / PER / 2; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] = __shfl_sync(0xffffffffu, k, 8 * i);
+}
+
+// A CTA has one row at a time; where a row takes one warp, four.
+__host__ __device__ constexpr int threads_of(int tpr) { return tpr < 64 ? 128 : tpr; }
 // CTAs of `threads` threads that share an SM when each thread may have `regs` registers.
 __host__ __device__ constexpr int ctas_of(int threads, int regs) { return 65536 / regs / threads < 1 ? 1 : 65536 / regs / threads; }
-__host__ __device__ constexpr int threads_of(int tpr) { return tpr < 128 ? 128 : tpr; }
-// Registers a thread of the forward kernel: a warp that has a row to itself has several runs' values in flight.
-__host__ __device__ constexpr int join_regs(int tpr) { return tpr == 32 ? 128 : 64; }
+// Registers a thread, forward and backward.  Two CTAs of 512 threads share an SM in the forward pass (4096 columns; one and
+// a half times as many registers, 96, 25.1 against 24.7 us, fewer, 42, 34), one in the backward one (64 registers 70 us
+// against 42.9).  Two runs a thread instead: forward 25.1, backward 65 us at 128 registers, 44 at 168.
+__host__ __device__ constexpr int join_regs() { return 64; }
+__host__ __device__ constexpr int grad_regs(int tpr) { return tpr == 1024 ? 64 : 128; }
+
 // What a column needs of the weights: the post-norm's times the channel's gate, and the pre-norm's.
-template <int V>
-struct ColumnWeights {
-    float p[V][8], q[V][8];
-    __device__ __forceinline__ void load(const JoinArgs& a, int i, int c) {
-        float k[8];
-        weights8(a.post ? a.w_post : nullptr, a.w_f32, c, p[i]);
-        weights8(a.gate_kind == DYNAMO_GATE_CHANNEL ? a.gate : nullptr, a.w_f32, c, k);
+__device__ __forceinline__ void post_weights(const JoinArgs& a, int c, F2 (&p)[4]) {
+    float w[8], k[8];
+    weights8(a.post ? a.w_post : nullptr, a.w_f32, c, w);
+    weights8(a.gate_kind == DYNAMO_GATE_CHANNEL ? a.gate : nullptr, a.w_f32, c, k);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[i][j] *= k[j];
-        weights8(a.w_pre, a.w_f32, c, q[i]);
-    }
-};
+    for (int j = 0; j < 4; ++j) p[j] = f2(w[2 * j] * k[2 * j], w[2 * j + 1] * k[2 * j + 1]);
+}
+__device__ __forceinline__ void pre_weights(const JoinArgs& a, int c, F2 (&q)[4]) {
+    float w[8];
+    weights8(a.w_pre, a.w_f32, c, w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = f2(w[2 * j], w[2 * j + 1]);
+}
 
 // TPR threads a row, V runs of eight columns a thread (run i of thread t: columns 8 (t + i TPR)).  The CTAs that the SMs hold walk
-// the rows, each thread with its columns' weights in registers and the next row on its way while it works on the present
-// one: at 4096 columns the weights are half as many bytes again as a row's, and with a CTA a row, that read them for it,
-// 4096 rows took 36.7 us.  KEEP = false (rows too wide for that): both are read when they are used.
+// the rows, each thread with its columns' weights in registers and the next row on its way while it works on the present one.
+// What bounds it is instructions as much as memory: two columns an instruction (f32x2).  4096 rows of 4096, bf16, gate per
+// channel: 24.7 us, 5.4 TB/s of rows; 36.7 with a CTA a row that read the weights for it (half as many bytes again as the
+// row's), 30.9 with one column an instruction.
+// KEEP = false (rows too wide for that): weights and rows are read when they are used.
 template <typename TY, typename TR, int TPR, int V, bool KEEP>
-__global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), join_regs(TPR))) norm_join_kernel(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), join_regs()))
+    norm_join_kernel(const __grid_constant__ JoinArgs a) {
     constexpr int THREADS = threads_of(TPR), ROWS = THREADS / TPR, W = TPR / 32;
-    __shared__ __align__(16) float scratch[2][W < 4 ? 4 : W];
+    __shared__ float scratch[2][W];
     pdl_prologue();
     const int tt = threadIdx.x % TPR, d = a.d;
     const float inv_d = 1.f / (float)d;
-    ColumnWeights<V> w;
-    if constexpr (KEEP)
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (8 * (tt + i * TPR) < d) w.load(a, i, 8 * (tt + i * TPR));
-    Raw8<TY> yr[V], yn[V];
-    Raw8<TR> rr[V], rn[V];
-    auto fetch = [&](Raw8<TY> (&y)[V], Raw8<TR> (&r)[V], long long t) {
+    F2 p[V][4], q[V][4];
+    struct Row {
+        Raw8<TY> y[V];
+        Raw8<TR> r[V];
+        float gt;
+    };
+    auto fetch = [&](Row& R, long long t) {
+        const bool there = t < a.T;
+        R.gt = there && a.gate_kind == DYNAMO_GATE_TOKEN ? ((const float*)a.gate)[t] : 1.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = 8 * (tt + i * TPR);
-            const bool in = t < a.T && c < d;
-            y[i] = a.y && in ? load8((const TY*)a.y + t * d + c) : zero8<TY>();
-            r[i] = in ? load8((const TR*)a.r + t * d + c) : zero8<TR>();
+            const bool in = there && c < d;
+            R.y[i] = a.y && in ? load8((const TY*)a.y + t * d + c) : zero8<TY>();
+            R.r[i] = in ? load8((const TR*)a.r + t * d + c) : zero8<TR>();
         }
     };
     const long long step = (long long)gridDim.x * ROWS;
     long long t = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
-    if constexpr (KEEP) fetch(yn, rn, t);
-    for (; t < a.T; t += step) {
-        if constexpr (KEEP) {
+    Row R;
+    fetch(R, t);
+    if constexpr (KEEP)
 #pragma unroll
-            for (int i = 0; i < V; ++i) yr[i] = yn[i], rr[i] = rn[i];
-            fetch(yn, rn, t + step);
-        } else {
-            fetch(yr, rr, t);
+        for (int i = 0; i < V; ++i)
+            if (8 * (tt + i * TPR) < d) {
+                post_weights(a, 8 * (tt + i * TPR), p[i]);
+                pre_weights(a, 8 * (tt + i * TPR), q[i]);
+            }
+    const F2 res = f2(a.y ? a.res_scale : 1.f);
+    for (; t < a.T; t += step) {
+        F2 y[V][4], x[V][4];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            unpack8(R.y[i], y[i]);
+            unpack8(R.r[i], x[i]);
         }
-        const float gt = a.gate_kind == DYNAMO_GATE_TOKEN ? ((const float*)a.gate)[t] : 1.f;
+        const float gate = a.block_scale * R.gt;
+        if constexpr (KEEP) fetch(R, t + step);   // on its way from here on, into the registers that were just read
         float s_y = 1.f;
         if (a.post) {
-            float sum[1] = {0.f};
+            F2 sum2 = f2(0.f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float y[8];
-                unpack8(yr[i], y);
+            for (int i = 0; i < V; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[0] = fmaf(y[j], y[j], sum[0]);
-            }
-            row_sums<TPR, 1>(sum, scratch[0]);
-            s_y = rsqrtf(fmaf(sum[0], inv_d, a.eps));
+                for (int j = 0; j < 4; ++j) sum2 = fma2(y[i][j], y[i][j], sum2);
+            s_y = rsqrtf(fmaf(row_sum<TPR>(lo(sum2) + hi(sum2), scratch[0]), inv_d, a.eps));
         }
-        const float g = a.block_scale * gt * s_y;
-        float x[V][8];
-        float sum[1] = {0.f};
+        const F2 g = f2(gate * s_y);
+        F2 sum2 = f2(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = 8 * (tt + i * TPR);
-            unpack8(rr[i], x[i]);
             if (a.y && c < d) {
-                float y[8];
-                unpack8(yr[i], y);
-                if constexpr (!KEEP) w.load(a, i, c);
+                if constexpr (!KEEP) post_weights(a, c, p[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[i][j] = fmaf(g, w.p[i][j] * y[j], a.res_scale * x[i][j]);
+                for (int j = 0; j < 4; ++j) x[i][j] = fma2(g, mul2(p[i][j], y[i][j]), mul2(res, x[i][j]));
                 store8((TR*)a.r_out + t * d + c, x[i]);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[0] = fmaf(x[i][j], x[i][j], sum[0]);
+            for (int j = 0; j < 4; ++j) sum2 = fma2(x[i][j], x[i][j], sum2);
         }
         float s_r = 1.f;
         if (a.pre) {
-            row_sums<TPR, 1>(sum, scratch[1]);
-            s_r = rsqrtf(fmaf(sum[0], inv_d, a.eps));
+            s_r = rsqrtf(fmaf(row_sum<TPR>(lo(sum2) + hi(sum2), scratch[1]), inv_d, a.eps));
+            const F2 s2 = f2(s_r);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = 8 * (tt + i * TPR);
                 if (c >= d) continue;
-                float n[8];
-                if constexpr (KEEP) {
+                if constexpr (!KEEP) pre_weights(a, c, q[i]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) n[j] = w.q[i][j];
-                } else {
-                    weights8(a.w_pre, a.w_f32, c, n);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) n[j] *= x[i][j] * s_r;
-                if (a.n_f32) store8((float*)a.n_out + t * d + c, n);
-                else store8((__nv_bfloat16*)a.n_out + t * d + c, n);
+                for (int j = 0; j < 4; ++j) x[i][j] = mul2(q[i][j], mul2(x[i][j], s2));
+                if (a.n_f32) store8((float*)a.n_out + t * d + c, x[i]);
+                else store8((__nv_bfloat16*)a.n_out + t * d + c, x[i]);
             }
         }
         if (a.stats && tt == 0) *reinterpret_cast<float2*>(a.stats + 2 * t) = make_float2(s_y, s_r);
+        if constexpr (!KEEP) fetch(R, t + step);
         // One reduction a row alone would use the same scratch for the next row's: its readers have to be through.
         if constexpr (TPR > 32)
             if (!(a.post && a.pre)) __syncthreads();
     }
 }
 
-// The gradient, laid out the same.  The column sums of d_w_post and of a channel gate differ by a factor of the column
+// The gradient, laid out the same.  What the first pass over a row has worked out in fp32 (r', dr' + s_r u, y, dn) stays in
+// registers for the second; the next row's loads go out once it has read the present one's registers.  4096 rows of 4096, bf16,
+// gate per channel: 42.9 us with the launch that adds up the CTAs' sums (4.7 TB/s); 47 with every sum reduced by itself and a
+// copy of the row that came, 56 with the rows staged in shared memory and read twice.  The column sums of d_w_post and of a channel gate differ by a factor of the column
 // (S1 = sum_t block_scale gate_t G y s_y; d_w_post = gate S1, d_gate = w_post S1), so that two sums a column are kept.
 template <typename TY, typename TR, typename TN, int TPR, int V, bool KEEP>
-__global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), 128)) norm_join_grad_kernel(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), grad_regs(TPR)))
+    norm_join_grad_kernel(const __grid_constant__ JoinArgs a) {
     constexpr int THREADS = threads_of(TPR), ROWS = THREADS / TPR, W = TPR / 32;
-    __shared__ __align__(16) float scratch[2][3 * (W < 4 ? 4 : W)];
-    extern __shared__ float s_sum[];   // several rows a CTA: [2][d] for the CTA's column sums
+    __shared__ float scratch[2][4 * W];
+    extern __shared__ __align__(16) float s_sum[];   // several rows a CTA: [2][d] for the CTA's column sums
     pdl_prologue();
     const int tt = threadIdx.x % TPR, d = a.d, row0 = threadIdx.x / TPR;
     const float inv_d = 1.f / (float)d;
-    float acc[2][V][8];
+    F2 acc[2][V][4];
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[q][i][j] = 0.f;
-    ColumnWeights<V> w;
-    if constexpr (KEEP)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (8 * (tt + i * TPR) < d) w.load(a, i, 8 * (tt + i * TPR));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[k][i][j] = f2(0.f);
+    F2 p[V][4], q[V][4];
     struct Row {
         Raw8<TY> y[V];
         Raw8<TR> r[V], dr[V];
         Raw8<TN> dn[V];
-        float2 st;
-        float gt;
+        float s_y, s_r, gt;
     };
     auto fetch = [&](Row& R, long long t) {
         const bool there = t < a.T;
-        R.st = there ? *reinterpret_cast<const float2*>(a.stats + 2 * t) : make_float2(1.f, 1.f);
+        const float2 st = there ? *reinterpret_cast<const float2*>(a.stats + 2 * t) : make_float2(1.f, 1.f);
+        R.s_y = a.post ? st.x : 1.f;
+        R.s_r = st.y;
         R.gt = there && a.gate_kind == DYNAMO_GATE_TOKEN ? ((const float*)a.gate)[t] : 1.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -248,93 +310,105 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), 128)
     };
     const long long step = (long long)gridDim.x * ROWS;
     long long t = (long long)blockIdx.x * ROWS + row0;
-    Row R, next;
-    if constexpr (KEEP) fetch(next, t);
-    const float res = a.y ? a.res_scale : 1.f;
+    Row R;
+    fetch(R, t);
+    if constexpr (KEEP)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (8 * (tt + i * TPR) < d) {
+                post_weights(a, 8 * (tt + i * TPR), p[i]);
+                pre_weights(a, 8 * (tt + i * TPR), q[i]);
+            }
+    const F2 res = f2(a.y ? a.res_scale : 1.f);
     int turn = 0;
     for (; t < a.T; t += step, turn ^= 1) {
-        if constexpr (KEEP) {
-            R = next;
-            fetch(next, t + step);
-        } else {
-            fetch(R, t);
-        }
-        const float s_y = a.post ? R.st.x : 1.f, s_r = R.st.y, gz = a.block_scale * R.gt;
-        // sums over the row: A = u r', B = k z (dr' + s_r u), C = k z r' with k the gate of the channels (the token's and
-        // block_scale are put in afterwards)
-        float sum[3] = {0.f, 0.f, 0.f};
+        const float s_y = R.s_y, s_r = R.s_r, gz = a.block_scale * R.gt;
+        F2 y[V][4], x[V][4], g[V][4], dn[V][4];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int c = 8 * (tt + i * TPR);
-            if (c >= d) continue;
-            if constexpr (!KEEP) w.load(a, i, c);
-            float y[8], r[8], g[8], dn[8];
-            unpack8(R.y[i], y);
-            unpack8(R.r[i], r);
-            unpack8(R.dr[i], g);
-            unpack8(R.dn[i], dn);
+            unpack8(R.y[i], y[i]);
+            unpack8(R.r[i], x[i]);
+            unpack8(R.dr[i], g[i]);
+            unpack8(R.dn[i], dn[i]);
+        }
+        if constexpr (KEEP) fetch(R, t + step);   // on its way from here on, into the registers that were just read
+        // sums over the row: A = u r', B = k z (dr' + s_r u), C = k z r' with k the gate of the channels (the token's and
+        // block_scale are put in afterwards); k z = s_y (p y)
+        F2 sum2[3] = {f2(0.f), f2(0.f), f2(0.f)};
+        {
+            const F2 gy2 = f2(gz * s_y), sr2 = f2(s_r);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float kz = w.p[i][j] * (y[j] * s_y);
-                const float x = fmaf(gz, kz, res * r[j]);
-                const float u = w.q[i][j] * dn[j];
-                sum[0] = fmaf(u, x, sum[0]);
-                sum[1] = fmaf(kz, fmaf(s_r, u, g[j]), sum[1]);
-                sum[2] = fmaf(kz, x, sum[2]);
+            for (int i = 0; i < V; ++i) {
+                const int c = 8 * (tt + i * TPR);
+                if (c >= d) continue;
+                if constexpr (!KEEP) {
+                    post_weights(a, c, p[i]);
+                    pre_weights(a, c, q[i]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const F2 py = mul2(p[i][j], y[i][j]);
+                    x[i][j] = fma2(gy2, py, mul2(res, x[i][j]));
+                    const F2 u = mul2(q[i][j], dn[i][j]);
+                    g[i][j] = fma2(sr2, u, g[i][j]);
+                    sum2[0] = fma2(u, x[i][j], sum2[0]);
+                    sum2[1] = fma2(py, g[i][j], sum2[1]);
+                    sum2[2] = fma2(py, x[i][j], sum2[2]);
+                }
             }
         }
-        row_sums<TPR, 3>(sum, scratch[turn]);
+        float sum[3] = {lo(sum2[0]) + hi(sum2[0]), lo(sum2[1]) + hi(sum2[1]), lo(sum2[2]) + hi(sum2[2])};
+        row_sums<TPR>(sum, scratch[turn]);
         const float ca = s_r * s_r * s_r * inv_d * sum[0];      // G = dr' + s_r u - ca r'
-        const float zg = sum[1] - ca * sum[2];                  // sum(k z G)
+        const float zg = s_y * (sum[1] - ca * sum[2]);          // sum(k z G)
         if (a.d_gate && a.gate_kind == DYNAMO_GATE_TOKEN && tt == 0) a.d_gate[t] = a.block_scale * zg;
         const float cv = a.post ? gz * zg * inv_d : 0.f;        // sum(v y) s_y / d
+        const F2 ca2 = f2(-ca), gy2 = f2(gz * s_y), cy2 = f2(-cv * s_y * s_y), sr2 = f2(s_r);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = 8 * (tt + i * TPR);
             if (c >= d) continue;
-            if constexpr (!KEEP) w.load(a, i, c);
-            float y[8], r[8], g[8], dn[8];
-            unpack8(R.y[i], y);
-            unpack8(R.r[i], r);
-            unpack8(R.dr[i], g);
-            unpack8(R.dn[i], dn);
+            if constexpr (!KEEP) post_weights(a, c, p[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float yn = y[j] * s_y;
-                const float x = fmaf(gz, w.p[i][j] * yn, res * r[j]);
-                const float G = fmaf(-ca, x, fmaf(s_r, w.q[i][j] * dn[j], g[j]));
-                const float gG = gz * G;
-                r[j] = res * G;
-                y[j] = s_y * fmaf(-cv, yn, w.p[i][j] * gG);
-                acc[0][i][j] = fmaf(gG, yn, acc[0][i][j]);
-                acc[1][i][j] = fmaf(dn[j], x * s_r, acc[1][i][j]);
+            for (int j = 0; j < 4; ++j) {
+                const F2 G = fma2(ca2, x[i][j], g[i][j]);
+                const F2 gG = mul2(gy2, G);
+                acc[0][i][j] = fma2(gG, y[i][j], acc[0][i][j]);
+                acc[1][i][j] = fma2(dn[i][j], mul2(x[i][j], sr2), acc[1][i][j]);
+                y[i][j] = fma2(p[i][j], gG, mul2(cy2, y[i][j]));
+                g[i][j] = mul2(res, G);
             }
-            if (a.d_r) store8((TR*)a.d_r + t * d + c, r);
-            if (a.d_y) store8((TY*)a.d_y + t * d + c, y);
+            if (a.d_r) store8((TR*)a.d_r + t * d + c, g[i]);
+            if (a.d_y) store8((TY*)a.d_y + t * d + c, y[i]);
         }
+        if constexpr (!KEEP) fetch(R, t + step);
     }
     if (!a.part) return;
     float* part = a.part + (long long)blockIdx.x * 2 * d;
     if constexpr (ROWS == 1) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = 8 * (tt + i * TPR);
-                if (c < d) store8(part + q * d + c, acc[q][i]);
+                if (c < d) store8(part + k * d + c, acc[k][i]);
             }
     } else {
         // the CTA's rows one after another: the order of the sum is fixed
         for (int o = 0; o < ROWS; ++o) {
             if (row0 == o)
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const int c = 8 * (tt + i * TPR);
                         if (c >= d) continue;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) s_sum[q * d + c + j] = (o ? s_sum[q * d + c + j] : 0.f) + acc[q][i][j];
+                        for (int j = 0; j < 4; ++j) {
+                            float2* at = reinterpret_cast<float2*>(s_sum + k * d + c + 2 * j);
+                            const float2 was = o ? *at : make_float2(0.f, 0.f);
+                            *at = make_float2(was.x + lo(acc[k][i][j]), was.y + hi(acc[k][i][j]));
+                        }
                     }
             __syncthreads();
         }
@@ -344,20 +418,20 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), 128)
 
 // Column sums of the CTAs' partial rows, in a fixed order, and the factors of the two gradients that share one.  grid.y: which
 // of the two sums.
-__global__ void __launch_bounds__(256) norm_join_sums_kernel(const __grid_constant__ JoinArgs a, int n_part, float* d_w_post,
+__global__ void __launch_bounds__(1024) norm_join_sums_kernel(const __grid_constant__ JoinArgs a, int n_part, float* d_w_post,
                                                              float* d_gate, float* d_w_pre) {
-    __shared__ float s[8][32];
+    __shared__ float s[32][32];
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, d = a.d;
     float sum = 0.f;
     if (c < d)
 #pragma unroll 8
-        for (int p = warp; p < n_part; p += 8) sum += a.part[((long long)p * 2 + blockIdx.y) * d + c];
+        for (int p = warp; p < n_part; p += 32) sum += a.part[((long long)p * 2 + blockIdx.y) * d + c];
     s[warp][lane] = sum;
     __syncthreads();
     if (warp || c >= d) return;
 #pragma unroll
-    for (int w = 1; w < 8; ++w) sum += s[w][lane];
+    for (int w = 1; w < 32; ++w) sum += s[w][lane];
     if (blockIdx.y) {
         if (d_w_pre) d_w_pre[c] = sum;
         return;
@@ -369,8 +443,8 @@ __global__ void __launch_bounds__(256) norm_join_sums_kernel(const __grid_consta
 
 constexpr int JOIN_MAX_D = 16384;
 
-// Threads a row and runs a thread by the width: a warp where its four runs cover the row (no barrier), else as many threads as
-// there are runs, up to the 1024 of a CTA.
+// Threads a row and runs a thread by the width: a run a thread as far as registers allow, one warp a row (no barrier) while
+// that is enough.
 template <int TPR_, int V_, bool KEEP_>
 struct Layout {
     static constexpr int TPR = TPR_, V = V_;
@@ -379,11 +453,14 @@ struct Layout {
 template <bool GRAD, typename F>
 static cudaError_t by_width(int d, F f) {
     if (d <= 256) return f(Layout<32, 1, true>{});
-    if (d <= 512) return f(Layout<32, 2, !GRAD>{});
+    if (d <= 512) return f(Layout<64, 1, true>{});
     if (d <= 1024) return f(Layout<128, 1, true>{});
     if (d <= 2048) return f(Layout<256, 1, true>{});
     if (d <= 4096) return f(Layout<512, 1, true>{});
-    if (d <= 8192) return f(Layout<1024, 1, !GRAD>{});
+    if (d <= 8192) {
+        if constexpr (GRAD) return f(Layout<512, 2, false>{});
+        else return f(Layout<1024, 1, true>{});
+    }
     return f(Layout<1024, 2, false>{});
 }
 template <typename F>
@@ -393,15 +470,15 @@ static cudaError_t by_types(int a, int b, F f) {
 }
 
 // CTAs of a launch: what the SMs hold at once, and no more than there are rows.
-template <typename L>
-static int ctas_for(int T, int regs, int n_sms) {
-    constexpr int THREADS = threads_of(L::TPR), ROWS = THREADS / L::TPR;
-    return (int)std::max(1ll, std::min({((long long)T + ROWS - 1) / ROWS, (long long)n_sms * ctas_of(THREADS, regs)}));
+static int join_ctas(int T, int tpr, int per_sm, int n_sms) {
+    const int rows = threads_of(tpr) / tpr;
+    return (int)std::max(1ll, std::min(((long long)T + rows - 1) / rows, (long long)n_sms * per_sm));
 }
 static int grad_ctas(int T, int d, int n_sms) {
     int n = 0;
     by_width<true>(d, [&](auto l) {
-        n = ctas_for<decltype(l)>(T, 128, n_sms);
+        constexpr int TPR = decltype(l)::TPR;
+        n = join_ctas(T, TPR, ctas_of(threads_of(TPR), grad_regs(TPR)), n_sms);
         return cudaSuccess;
     });
     return n;
@@ -472,8 +549,9 @@ dynamo_status dynamo_norm_join_forward(const dynamo_join_desc* desc, const void*
         using TR = std::remove_pointer_t<decltype(tr)>;
         return by_width<false>(desc->d, [&](auto l) {
             using L = decltype(l);
-            return launch_pdl(norm_join_kernel<TY, TR, L::TPR, L::V, L::KEEP>, dim3((unsigned)ctas_for<L>(T, join_regs(L::TPR), n_sms)),
-                              dim3(threads_of(L::TPR)), 0, (cudaStream_t)stream, a);
+            constexpr int THREADS = threads_of(L::TPR), PER_SM = ctas_of(THREADS, join_regs());
+            return launch_pdl(norm_join_kernel<TY, TR, L::TPR, L::V, L::KEEP>, dim3((unsigned)join_ctas(T, L::TPR, PER_SM, n_sms)),
+                              dim3(THREADS), 0, (cudaStream_t)stream, a);
         });
     });
     return e == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;
@@ -524,13 +602,13 @@ dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void
         return by_width<true>(desc->d, [&](auto l) {
             using L = decltype(l);
             const dim3 grid((unsigned)ctas), block(threads_of(L::TPR));
-            const size_t smem = L::TPR < 128 ? 2 * desc->d * sizeof(float) : 0;
+            const size_t smem = threads_of(L::TPR) > L::TPR ? 2 * desc->d * sizeof(float) : 0;
             return a.n_f32 ? launch_pdl(norm_join_grad_kernel<TY, TR, float, L::TPR, L::V, L::KEEP>, grid, block, smem, st, a)
                            : launch_pdl(norm_join_grad_kernel<TY, TR, __nv_bfloat16, L::TPR, L::V, L::KEEP>, grid, block, smem, st, a);
         });
     });
     if (e != cudaSuccess) return DYNAMO_ERR_CUDA;
-    if (columns && launch_pdl(norm_join_sums_kernel, dim3((unsigned)((desc->d + 31) / 32), 2), dim3(256), 0, st, a, ctas,
+    if (columns && launch_pdl(norm_join_sums_kernel, dim3((unsigned)((desc->d + 31) / 32), 2), dim3(1024), 0, st, a, ctas,
                               d_w_post, channel ? d_gate : nullptr, d_w_pre) != cudaSuccess)
         return DYNAMO_ERR_CUDA;
     return DYNAMO_OK;
