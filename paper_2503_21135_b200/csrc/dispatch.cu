@@ -14,7 +14,7 @@
 namespace dyn {
 
 constexpr int DISPATCH_EXPERTS = 256;
-constexpr int DISPATCH_THREADS = 256;
+constexpr int DISPATCH_THREADS = 1024;
 constexpr int DISPATCH_WARPS = DISPATCH_THREADS / 32;
 constexpr int DISPATCH_CHUNK = 2048;      // pairs that a CTA ranks at a time
 
@@ -27,77 +27,101 @@ struct DispatchArgs {
     const uint8_t* x;      // rows of row_bytes, or NULL: sort alone
     uint8_t* rows;
     long long row_bytes;
-    int32_t* hist;         // [CTA][E] pairs of each CTA's tokens by expert, or NULL: every CTA counts the whole array
+    int32_t* hist;         // [CTA][E_pad] pairs of each CTA's tokens by expert, or NULL: every CTA counts the whole array
+    int E_pad;             // E rounded up to a power of two
 };
 
-// Counts of the pairs [lo, hi) by expert into shared counters (integer additions: any order gives the same counts).
-__device__ __forceinline__ void count_pairs(const int32_t* __restrict__ idx, long long lo, long long hi, int E, int* counts) {
-    for (long long i = lo + threadIdx.x; i < hi; i += DISPATCH_THREADS) {
-        const uint32_t e = (uint32_t)idx[i];
-        if (e < (uint32_t)E) atomicAdd(counts + e, 1);
+// Counts of the pairs [lo, hi) by expert into shared counters, those in front of `mid` into `before`, the others into `behind`
+// (integer additions: any order gives the same counts).  Sixteen bytes of indices a load where the array's address allows.
+__device__ __forceinline__ void count_pairs(const int32_t* __restrict__ idx, long long lo, long long mid, long long hi, int E, int* before,
+                                            int* behind) {
+    auto count = [&](int v, long long i) {
+        if ((uint32_t)v < (uint32_t)E) atomicAdd((i < mid ? before : behind) + v, 1);
+    };
+    long long done = lo;
+    if ((((uintptr_t)idx + 4 * lo) & 15) == 0) {
+        const long long n4 = (hi - lo) / 4;
+#pragma unroll 4
+        for (long long q = threadIdx.x; q < n4; q += DISPATCH_THREADS) {
+            const int4 v = *reinterpret_cast<const int4*>(idx + lo + 4 * q);
+            count(v.x, lo + 4 * q);
+            count(v.y, lo + 4 * q + 1);
+            count(v.z, lo + 4 * q + 2);
+            count(v.w, lo + 4 * q + 3);
+        }
+        done = lo + 4 * n4;
     }
+    for (long long i = done + threadIdx.x; i < hi; i += DISPATCH_THREADS) count(idx[i], i);
 }
 
-__global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(DispatchArgs a) {
+__global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const __grid_constant__ DispatchArgs a) {
     __shared__ int s_count[DISPATCH_EXPERTS];
     pdl_prologue();
-    s_count[threadIdx.x] = 0;
+    if (threadIdx.x < DISPATCH_EXPERTS) s_count[threadIdx.x] = 0;
     __syncthreads();
     const long long lo = (long long)blockIdx.x * a.seg * a.k, hi = min((long long)a.T * a.k, lo + (long long)a.seg * a.k);
-    count_pairs(a.idx, lo, hi, a.E, s_count);
+    count_pairs(a.idx, lo, lo, hi, a.E, s_count, s_count);
     __syncthreads();
-    if (threadIdx.x < a.E) a.hist[(long long)blockIdx.x * a.E + threadIdx.x] = s_count[threadIdx.x];
+    if (threadIdx.x < a.E_pad) a.hist[blockIdx.x * a.E_pad + threadIdx.x] = s_count[threadIdx.x];
 }
 
-// One CTA per run of `seg` tokens.  First the experts' totals and the pairs of each expert in front of the run, then the
-// run's pairs are ranked (a warp per contiguous piece, lanes of the same expert found by match.any: the order is that of
-// the pairs) and its tokens' rows copied, one read and k writes each.
-__global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_kernel(DispatchArgs a) {
+// One CTA per run of `seg` tokens, one an SM.  First the experts' totals and the pairs of each expert in front of the run, then
+// the run's pairs are ranked (a warp per contiguous piece, lanes of the same expert found by match.any: the order is that of
+// the pairs) and its tokens' rows copied, one read and k writes each, 16 bytes a thread and four of them at a time.
+// Every CTA counts the whole array, so one of 1024 threads an SM: 4096 tokens of 8 KB, top-2 of 8 experts, 21.8 us (4.6 TB/s;
+// some 4 us of it in front of the first copy), 24.2 with four CTAs of 256.  Asking for the rows ahead of the count (into the
+// L2, 64 to 256 KB a CTA) made it 22.5, eight pieces a thread at a time 22.2: it is the writes that bound it.
+__global__ void __launch_bounds__(DISPATCH_THREADS, 1) dispatch_kernel(const __grid_constant__ DispatchArgs a) {
     __shared__ int s_total[DISPATCH_EXPERTS], s_next[DISPATCH_EXPERTS];
     __shared__ int s_hist[DISPATCH_WARPS][DISPATCH_EXPERTS];
     __shared__ int s_pos[DISPATCH_CHUNK];
-    __shared__ int s_warp[DISPATCH_WARPS];
+    __shared__ int s_warp[DISPATCH_EXPERTS / 32];
     pdl_prologue();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int k = a.k, E = a.E;
     const long long n_pairs = (long long)a.T * k;
     const int t0 = blockIdx.x * a.seg, t1 = min(a.T, t0 + a.seg);
     const long long lo = (long long)t0 * k;
-    s_total[tid] = 0;
-    s_next[tid] = 0;
+    if (tid < DISPATCH_EXPERTS) {
+        s_total[tid] = 0;
+        s_next[tid] = 0;
+    }
     __syncthreads();
     if (a.hist) {
-        const int mine = blockIdx.x * E, all = gridDim.x * E;
+        // a thread adds up every (threads / E_pad)-th CTA's count of one expert
+        const int e = tid & (a.E_pad - 1);
+        int before = 0, behind = 0;
 #pragma unroll 8
-        for (int i = tid; i < all; i += DISPATCH_THREADS) {
-            const int c = a.hist[i];
-            if (c) {
-                const int e = i % E;
-                atomicAdd(s_total + e, c);
-                if (i < mine) atomicAdd(s_next + e, c);
-            }
+        for (int r = tid / a.E_pad; r < (int)gridDim.x; r += DISPATCH_THREADS / a.E_pad) {
+            const int c = a.hist[r * a.E_pad + e];
+            (r < (int)blockIdx.x ? before : behind) += c;
         }
+        if (before) atomicAdd(s_next + e, before);
+        if (behind) atomicAdd(s_total + e, behind);
     } else {
-        count_pairs(a.idx, 0, lo, E, s_next);
-        count_pairs(a.idx, lo, n_pairs, E, s_total);
+        count_pairs(a.idx, 0, lo, n_pairs, E, s_next, s_total);
     }
     __syncthreads();
     // exclusive scan of the totals, an expert per thread
-    int total = s_total[tid] + (a.hist ? 0 : s_next[tid]), sum = total;
+    int total = 0, sum = 0;
+    if (tid < DISPATCH_EXPERTS) {
+        total = sum = s_total[tid] + s_next[tid];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += u;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += u;
+        }
+        if (lane == 31) s_warp[warp] = sum;
     }
-    if (lane == 31) s_warp[warp] = sum;
     __syncthreads();
-    int before = 0;
-    for (int w = 0; w < warp; ++w) before += s_warp[w];
-    const int first = before + sum - total;     // first row of expert tid
-    s_next[tid] += first;                        // its first row of this run
-    if (blockIdx.x == 0) {
-        if (tid < E) a.offsets[tid] = first;
-        if (tid == E - 1) a.offsets[E] = first + total;
+    if (tid < DISPATCH_EXPERTS) {
+        int first = sum - total;                 // first row of expert tid
+        for (int w = 0; w < warp; ++w) first += s_warp[w];
+        s_next[tid] += first;                    // its first row of this run
+        if (blockIdx.x == 0) {
+            if (tid < E) a.offsets[tid] = first;
+            if (tid == E - 1) a.offsets[E] = first + total;
+        }
     }
     const unsigned lt = (1u << lane) - 1;
     const int chunk_tokens = DISPATCH_CHUNK / k;
@@ -106,19 +130,18 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_kernel(DispatchArgs
         const int n = (c1 - c0) * k;
         const long long base = (long long)c0 * k;
         const int piece = ((n + 31) / 32 + DISPATCH_WARPS - 1) / DISPATCH_WARPS * 32;   // whole batches of 32 a warp
+        const int pieces = (n + piece - 1) / piece;
         const int p0 = min(n, warp * piece), p1 = min(n, p0 + piece);
-#pragma unroll
-        for (int i = 0; i < DISPATCH_WARPS; ++i) s_hist[i][tid] = 0;
+        for (int i = tid; i < pieces * DISPATCH_EXPERTS; i += DISPATCH_THREADS) (&s_hist[0][0])[i] = 0;
         __syncthreads();
         for (int p = p0 + lane; p - lane < p1; p += 32) {
             const uint32_t e = p < p1 ? (uint32_t)a.idx[base + p] : 0xffffffffu;
             if (e < (uint32_t)E) atomicAdd(&s_hist[warp][e], 1);
         }
         __syncthreads();
-        {
+        if (tid < E) {
             int next = s_next[tid];
-#pragma unroll
-            for (int i = 0; i < DISPATCH_WARPS; ++i) {
+            for (int i = 0; i < pieces; ++i) {
                 const int c = s_hist[i][tid];
                 s_hist[i][tid] = next;
                 next += c;
@@ -144,26 +167,28 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_kernel(DispatchArgs
         }
         __syncthreads();
         if (a.x) {
-            // a warp per token and slice of its row
-            const int nt = c1 - c0, n_vec = (int)(a.row_bytes >> 4);
-            const int slices = min((n_vec + 31) / 32, (DISPATCH_WARPS + nt - 1) / nt);
-            const int per = (n_vec + slices - 1) / slices;
-            for (int item = warp; item < nt * slices; item += DISPATCH_WARPS) {
-                const int t = item / slices, v0 = (item - t * slices) * per, v1 = min(n_vec, v0 + per);
-                const uint4* src = reinterpret_cast<const uint4*>(a.x + (long long)(c0 + t) * a.row_bytes);
-                const int* at = s_pos + t * k;
-                for (int v = v0 + lane; v < v1; v += 128) {
-                    uint4 buf[4];
+            // thread's 16-byte piece v of token t, a CTA's width further each time
+            const int n_vec = (int)(a.row_bytes >> 4), items = (c1 - c0) * n_vec;
+            const int dt = DISPATCH_THREADS / n_vec, dv = DISPATCH_THREADS - dt * n_vec;
+            const uint4* src = reinterpret_cast<const uint4*>(a.x + (long long)c0 * a.row_bytes);
+            int t = tid / n_vec, v = tid - t * n_vec;
+            for (int item = tid; item < items; item += 4 * DISPATCH_THREADS) {
+                uint4 buf[4];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (v + 32 * u < v1) buf[u] = ld_stream(src + v + 32 * u);
-                    for (int j = 0; j < k; ++j) {
-                        const int r = at[j];
-                        if (r < 0) continue;
-                        uint4* dst = reinterpret_cast<uint4*>(a.rows + (long long)r * a.row_bytes);
+                for (int u = 0; u < 4; ++u)
+                    if (item + u * DISPATCH_THREADS < items) buf[u] = ld_stream(src + item + u * DISPATCH_THREADS);
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            if (v + 32 * u < v1) dst[v + 32 * u] = buf[u];
+                for (int u = 0; u < 4; ++u) {
+                    if (item + u * DISPATCH_THREADS < items)
+                        for (int j = 0; j < k; ++j) {
+                            const int r = s_pos[t * k + j];
+                            if (r >= 0) reinterpret_cast<uint4*>(a.rows + (long long)r * a.row_bytes)[v] = buf[u];
+                        }
+                    t += dt;
+                    v += dv;
+                    if (v >= n_vec) {
+                        v -= n_vec;
+                        ++t;
                     }
                 }
             }
@@ -206,16 +231,16 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const TI* __restrict_
     store8(y + (long long)t * d + c, acc);
 }
 
-// d_rows[pos[t,j]] = w[t,j] dy[t], d_w[t,j] = <rows[pos[t,j]], dy[t]>: both from one pass over the row of dy.  TPT threads a
-// token.
-template <typename TR, typename TY, int K, int TPT>
+// d_rows[pos[t,j]] = w[t,j] dy[t], d_w[t,j] = <rows[pos[t,j]], dy[t]>: both from one pass over the row of dy.  `tpt` threads a
+// token (a power of two up to 256).
+template <typename TR, typename TY, int K>
 __global__ void __launch_bounds__(256) combine_grad_kernel(const TY* __restrict__ dy, const TR* __restrict__ rows,
                                                            const int32_t* __restrict__ pos, const float* __restrict__ w,
-                                                           int T, int d, TR* __restrict__ d_rows, float* __restrict__ d_w) {
+                                                           int T, int d, int tpt, TR* __restrict__ d_rows, float* __restrict__ d_w) {
     __shared__ float s_part[8][K];
     pdl_prologue();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int t = blockIdx.x * (256 / TPT) + threadIdx.x / TPT, tt = threadIdx.x % TPT;
+    const int t = (int)((blockIdx.x * 256ll + threadIdx.x) / tpt), tt = threadIdx.x & (tpt - 1);
     float acc[K];
 #pragma unroll
     for (int j = 0; j < K; ++j) acc[j] = 0.f;
@@ -227,7 +252,7 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(const TY* __restrict_
             at[j] = place_of(pos[(long long)t * K + j], T * K);
             wt[j] = w ? w[(long long)t * K + j] : 1.f;
         }
-        for (int c = tt * 8; c < d; c += TPT * 8) {
+        for (int c = tt * 8; c < d; c += tpt * 8) {
             const Raw8<TY> g = load8(dy + (long long)t * d + c);
             Raw8<TR> raw[K];
 #pragma unroll
@@ -249,28 +274,24 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(const TY* __restrict_
         }
     }
     if (!d_w) return;
+    for (int o = min(tpt, 32) / 2; o; o >>= 1)
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
+        for (int j = 0; j < K; ++j) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
+    if (tpt <= 32) {
+        if (t < T && tt == 0)
 #pragma unroll
-        for (int o = 16; o; o >>= 1) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
+            for (int j = 0; j < K; ++j) d_w[(long long)t * K + j] = acc[j];
+        return;
     }
-    if constexpr (TPT == 32) {
-        if (t < T)
+    if (lane == 0)
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (lane == j) d_w[(long long)t * K + j] = acc[j];
-    } else {
-        if (lane == 0)
-#pragma unroll
-            for (int j = 0; j < K; ++j) s_part[warp][j] = acc[j];
-        __syncthreads();
-        if (t < T && tt < K) {
-            const int w0 = warp / (TPT / 32) * (TPT / 32);
-            float s = s_part[w0][tt];
-#pragma unroll
-            for (int i = 1; i < TPT / 32; ++i) s += s_part[w0 + i][tt];
-            d_w[(long long)t * K + tt] = s;
-        }
+        for (int j = 0; j < K; ++j) s_part[warp][j] = acc[j];
+    __syncthreads();
+    if (t < T && tt < K) {
+        const int w0 = threadIdx.x / tpt * (tpt / 32);
+        float s = s_part[w0][tt];
+        for (int i = 1; i < tpt / 32; ++i) s += s_part[w0 + i][tt];
+        d_w[(long long)t * K + tt] = s;
     }
 }
 
@@ -296,7 +317,6 @@ static cudaError_t by_types(int a, int b, F f) {
 
 // Up to this many pairs every CTA counts the whole array by itself; beyond, a launch in front counts each CTA's share.
 constexpr long long DISPATCH_ONE_PAIRS = 16384;
-constexpr int DISPATCH_CTAS_PER_SM = 4;
 
 }  // namespace dyn
 
@@ -321,8 +341,8 @@ dynamo_status dynamo_dispatch_workspace_bytes(int32_t T, int32_t n_experts, int3
     if (!bytes) return DYNAMO_ERR_NULL;
     if (n_experts < 1 || n_experts > DISPATCH_EXPERTS || top_k > n_experts) return DYNAMO_ERR_SHAPE;
     if (const dynamo_status s = check_route_sizes(T, top_k); s != DYNAMO_OK) return s;
-    // counts of every CTA, of which there are at most DISPATCH_CTAS_PER_SM an SM (up to 256 SMs are reckoned with)
-    *bytes = (long long)T * top_k > DISPATCH_ONE_PAIRS ? (size_t)256 * DISPATCH_CTAS_PER_SM * n_experts * 4 : 0;
+    // counts of every CTA, of which there is one an SM (up to 256 SMs are reckoned with)
+    *bytes = (long long)T * top_k > DISPATCH_ONE_PAIRS ? (size_t)256 * DISPATCH_EXPERTS * 4 : 0;
     return DYNAMO_OK;
 }
 
@@ -353,7 +373,9 @@ dynamo_status dynamo_dispatch(const int32_t* topk_idx, int32_t T, int32_t n_expe
     a.rows = (uint8_t*)rows;
     a.row_bytes = x ? (long long)d * (dtype == DYNAMO_BF16 ? 2 : 4) : 0;
     a.hist = need ? (int32_t*)workspace : nullptr;
-    const int most = std::min(256, n_sms) * DISPATCH_CTAS_PER_SM;
+    a.E_pad = 1;
+    while (a.E_pad < n_experts) a.E_pad *= 2;
+    const int most = std::min(256, n_sms);
     a.seg = std::max(1, (int)(((long long)T + most - 1) / most));
     const unsigned ctas = (unsigned)std::max(1, (int)(((long long)T + a.seg - 1) / a.seg));   // without tokens: the offsets
     if (a.hist && launch_pdl(dispatch_count_kernel, dim3(ctas), dim3(DISPATCH_THREADS), 0, st, a) != cudaSuccess)
@@ -391,18 +413,19 @@ dynamo_status dynamo_combine_backward(const void* dy, int32_t dy_dtype, const vo
     if (T == 0) return DYNAMO_OK;
     if (!dy || !rows || !pos || !d_rows) return DYNAMO_ERR_NULL;
     if (!aligned16(dy, rows, d_rows)) return DYNAMO_ERR_ALIGN;
+    // A run of eight columns a thread where there are few tokens, two where there are many (64 tokens of 2048, top-6: 2.7 and
+    // 4.1 us; 4096 of 1024: 23.7 with four runs, 20.5 with two).
+    const int runs = (long long)T * d < 8ll * 148 * 1024 ? 1 : 2;
+    int tpt = 1;
+    while (tpt < 256 && tpt * 8 * runs < d) tpt *= 2;
+    if (((long long)T * tpt + 255) / 256 > 0x7fffffffll) return DYNAMO_ERR_TOKENS;
     const cudaError_t e = by_types(dtype, dy_dtype, [&](auto* tr, auto* ty) {
         using TR = std::remove_pointer_t<decltype(tr)>;
         using TY = std::remove_pointer_t<decltype(ty)>;
         return by_top_k(top_k, [&](auto kc) {
             constexpr int K = decltype(kc)::value;
-            auto go = [&](auto tptc) {
-                constexpr int TPT = decltype(tptc)::value;
-                constexpr int PER = 256 / TPT;
-                return launch_pdl(combine_grad_kernel<TR, TY, K, TPT>, dim3((unsigned)((T + PER - 1) / PER)), dim3(256), 0,
-                                  (cudaStream_t)stream, (const TY*)dy, (const TR*)rows, pos, topk_w, T, d, (TR*)d_rows, d_w);
-            };
-            return d <= 1024 ? go(std::integral_constant<int, 32>{}) : go(std::integral_constant<int, 256>{});
+            return launch_pdl(combine_grad_kernel<TR, TY, K>, dim3((unsigned)(((long long)T * tpt + 255) / 256)), dim3(256), 0,
+                              (cudaStream_t)stream, (const TY*)dy, (const TR*)rows, pos, topk_w, T, d, tpt, (TR*)d_rows, d_w);
         });
     });
     return e == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;
