@@ -1,7 +1,8 @@
 """Build the C-ABI library ``libdynamo.so`` in-tree with nvcc for sm_100a (no GPU needed to compile).
 
 Every ``.cu`` file is compiled to its own object (in parallel; only the stale ones) and the objects are linked
-into the shared library.  No file uses relocatable device code, so plain ``-c`` objects link.
+into the shared library.  No file uses relocatable device code, so plain ``-c`` objects link.  ``torch_binding.cpp`` becomes
+an extension module beside it (``_native.so``), built with the host compiler against the installed torch's headers.
 """
 from __future__ import annotations
 
@@ -20,6 +21,8 @@ SOURCES = ["api.cu", "pack.cu", "route.cu", "switch.cu", "stats.cu", "ffn_stream
            "noalloc.cu", "assign.cu", "downside.cu", "debug.cu", "dispatch.cu", "norm_join.cu", "linear.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 CFLAGS = ARCH + ["-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
+NATIVE = os.path.join(HERE, "_native.so")
+NATIVE_SOURCE = "torch_binding.cpp"
 LFLAGS = ARCH + ["-shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
 
 
@@ -73,7 +76,36 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         want["__sources__"] = SOURCES
         with open(manifest_path, "w") as f:
             json.dump(want, f)
+    build_native(force)
     return LIB
+
+
+def build_native(force: bool = False) -> str:
+    """The extension module; built again when its source, the header or the installed torch or Python is another."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    manifest_path = os.path.join(OBJ, "native.json")
+    want = [_digest([os.path.join(CSRC, NATIVE_SOURCE), _headers()[-1]]), torch.__version__, sys.version]
+    try:
+        with open(manifest_path) as f:
+            have = json.load(f)
+    except (OSError, ValueError):
+        have = None
+    if force or have != want or not os.path.exists(NATIVE):
+        cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))) if os.path.sep in _nvcc() else "/usr/local/cuda"
+        include = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+        torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+        cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
+                f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"] + [f"-isystem{p}" for p in include] +
+               ["-o", NATIVE, os.path.join(CSRC, NATIVE_SOURCE), f"-L{HERE}", "-l:libdynamo.so", f"-L{torch_lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu",
+                "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
+        subprocess.check_call(cmd)
+        with open(manifest_path, "w") as f:
+            json.dump(want, f)
+    return NATIVE
 
 
 if __name__ == "__main__":
