@@ -456,12 +456,15 @@ dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void
  *   x bf16 [T, cols], y [T, rows] of y_dtype.  Products are exact, sums in fp32.  Made for the few rows of a decode step; the
  *   matrix is read once per 32 tokens at most.  An infinite or NaN activation makes its row NaN; the sum of 31 |x| over a group
  *   has to stay in the range of fp32.
+ * dynamo_linear_poll_status: synchronises the stream; DYNAMO_ERR_TIMEOUT if a bounded wait of dynamo_linear_forward expired on the
+ *   current device since the last call (the results concerned are NaN), else DYNAMO_OK.
  * group_size 64 or 128, cols a multiple of it up to 2^24, rows >= 1 (ERR_SHAPE); 0 <= T <= DYNAMO_LINEAR_MAX_TOKENS (ERR_TOKENS). */
 #define DYNAMO_LINEAR_MAX_TOKENS 65536
 dynamo_status dynamo_linear_quantize(const void* w, int32_t rows, int32_t cols, int32_t group_size, void* codes, void* params,
                                      void* stream);
 dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size,
                                     const void* codes, const void* params, void* y, int32_t y_dtype, void* stream);
+dynamo_status dynamo_linear_poll_status(void* stream);
 
 #ifdef __cplusplus
 }

@@ -13,7 +13,9 @@
 
 #include "../../include/dynamo.h"
 #include "common.cuh"
+#include "f32x2.cuh"
 #include "quant.cuh"
+#include "tcgen05.cuh"
 #include "vec8.cuh"
 
 namespace dyn {
@@ -295,186 +297,272 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
     cluster_sync_all();   // nobody leaves while others read its sums
 }
 
-// ---- more tokens: bound by the MMAs -----------------------------------------------------------------------------------------
-// CTA: 8 warps, 32 rows and 32 tokens each, TOK / 32 of them side by side along the tokens; a share of the input indices as
-// above.  A unit's codes, parameters and activations go through a ring in shared memory.  The activations are put into the order of
-// the codes' pairs on their way (load, byte permutes, store: a sixteenth of the permutes that every warp would do for itself); 16-byte
-// chunk `ch` (8 indices) of token t stands at chunk_at(t, ch), which lays the chunks that the four lanes of a row read at a time side by side
-// and the next token's beside them (no bank twice among eight lanes).  A warp's two atoms share each of its reads of them.
-// The activations' sums per group are one more n-tile's work a warp, left in shared memory for all.
-constexpr int LIN_STAGES = 3;
-template <int G>
-__device__ __forceinline__ int chunk_at(int t, int ch) {
-    using S = UnitShape<G>;
-    const int g = ch / (G / 8), in = ch % (G / 8), q = in / S::W, j = in % S::W;   // lane q's j-th chunk of group g
-    return t * 16 + ((q + 4 * (S::W * g + j)) ^ (4 * (t & 1)));
-}
-template <int G, int TOK>
-struct TileStage {
-    static constexpr int ROWS = 32 * LIN_WARPS / (TOK / 32);
-    uint4 x[TOK * 16];
-    uint4 code[ROWS * 4];
-    uint32_t param[UnitShape<G>::GROUPS][ROWS];
+// ---- tcgen05: the codes as the A operand in tensor memory -------------------------------------------------------------------
+// CTA: 128 rows, TOK tokens, a share of the groups; eight warps that all do the same.  Warp w has the lane quarter q = w % 4 of the
+// tensor memory: rows 32 q .., of which it expands 16 and folds all, half of the tokens (h = w / 4 says which).
+// A stage is one group:
+//   fill    codes of 16 rows -> 16 + q as bf16 pairs -> tensor memory (A, G / 2 columns; 16x256b, so that four lanes read a row's codes:
+//           a row a lane kept the L1 busy with 32 lines a load); the activations -> shared memory (B, K-major core matrices of 8 tokens x
+//           8 indices), in the order that this gives the indices, their sums by an mma.sync whose other operand is ones, from the
+//           registers that they came in; parameters of eight groups at a time -> shared memory
+//   MMAs    G / 16 tcgen05.mma of 128 x TOK x 16 into one of two accumulators, issued by one warp in one run, committed to a barrier
+//   fold    y += s * acc + (m - 16 s) * sum(x), two columns an instruction
+// Stage i + 1 is filled and its MMAs issued before stage i is folded: one barrier a stage, and the MMAs run under the next
+// stage's filling.  Two CTAs share an SM (each 256 columns of tensor memory at most, 128 registers a thread).
+// A poll of the MMAs' barrier is bounded; after an expired one the CTA's outputs are NaN and the status word is set.  The tensor
+// memory is given back before the CTAs of a cluster meet: nobody waits for another CTA while it holds some.
+constexpr int TC_ROWS = 128;
+static __device__ int32_t g_linear_status[16];
+
+template <int TOK, int G>
+struct TcShape {
+    static constexpr int OCTETS = TOK / 8, QUADS = G / 32;                       // eight tokens, 32 indices: a warp's task of the filling
+    static constexpr int TPW = OCTETS * QUADS < LIN_WARPS ? 1 : OCTETS * QUADS / LIN_WARPS;
+    static constexpr int SPLITS = QUADS / TPW;                                   // warps that share an octet: partial sums
+    static constexpr int LBO = TOK * 16 + 16;   // bytes between octets of indices; the pad keeps the filling's stores off one another's banks
+    static constexpr int XBUF = G / 8 * LBO;
+    static constexpr int W = G / 32;                                             // words of codes of a lane and row: a quarter of a group
+    static constexpr int A_COLS = G / 2, COLS = 2 * A_COLS + 2 * TOK <= 64 ? 64 : 2 * A_COLS + 2 * TOK <= 128 ? 128 : 256;
+    static constexpr int SMEM = 2 * XBUF > TOK * TC_ROWS * 4 ? 2 * XBUF : TOK * TC_ROWS * 4;
+    static_assert(2 * A_COLS + 2 * TOK <= COLS, "tensor memory");
 };
-__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+
+// The MMAs of a stage: G / 16 steps of 16 indices, A columns 8 k, B octets 2 k.  The first starts from zero.
+#define LIN_MMA(k, acc)                                                  \
+    "add.s64 bd, %2, " #k "*%4;\n\tadd.s32 aa, %1, " #k "*8;\n\t"        \
+    "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [aa], bd, %3, " acc ";\n\t"
+template <int G, int STEP>
+__device__ __forceinline__ void linear_mmas(uint32_t d, uint32_t a, uint64_t bd, uint32_t idesc, uint32_t bar) {
+    if constexpr (G == 128)
+        asm volatile(
+            "{\n\t.reg .pred q, p0, p1;\n\t.reg .b64 bd;\n\t.reg .b32 aa;\n\telect.sync _|q, 0xffffffff;\n\t"
+            "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t" LIN_MMA(0, "p0") LIN_MMA(1, "p1") LIN_MMA(2, "p1") LIN_MMA(3, "p1")
+                LIN_MMA(4, "p1") LIN_MMA(5, "p1") LIN_MMA(6, "p1") LIN_MMA(7, "p1")
+            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d), "r"(a), "l"(bd), "r"(idesc),
+            "n"(STEP), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q, p0, p1;\n\t.reg .b64 bd;\n\t.reg .b32 aa;\n\telect.sync _|q, 0xffffffff;\n\t"
+            "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t" LIN_MMA(0, "p0") LIN_MMA(1, "p1") LIN_MMA(2, "p1") LIN_MMA(3, "p1")
+            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d), "r"(a), "l"(bd), "r"(idesc),
+            "n"(STEP), "r"(bar)
+            : "memory");
 }
 __device__ __forceinline__ void cp_async4(void* dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
 }
+// Eight consecutive columns of the warp's 32 lanes, a row a lane.
+__device__ __forceinline__ void tc_ld_rows8(uint32_t at, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(at)
+                 : "memory");
+}
+
 template <int TOK, int G, typename TO>
-__global__ void __launch_bounds__(32 * LIN_WARPS, 2) linear_tile_kernel(const __grid_constant__ LinearArgs a) {
-    using S = UnitShape<G>;
-    using Stage = TileStage<G, TOK>;
-    constexpr int ROWS = Stage::ROWS, THREADS = 32 * LIN_WARPS, XC = TOK * 16 / THREADS, NT = 4;
-    extern __shared__ __align__(16) uint8_t smem[];
-    Stage* ring = reinterpret_cast<Stage*>(smem);
-    __shared__ __align__(8) float sums[2][S::GROUPS][TOK];
+__global__ void __launch_bounds__(32 * LIN_WARPS, 2) linear_tc_kernel(const __grid_constant__ LinearArgs a) {
+    using S = TcShape<TOK, G>;
+    constexpr int THREADS = 32 * LIN_WARPS, NC = TOK / 2, W = S::W;   // NC: columns that a warp folds
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) float sums[3][S::SPLITS][TOK];
+    __shared__ uint32_t params[2][8][TC_ROWS];   // of eight groups, and of the next eight
+    __shared__ uint64_t bars[2];
+    __shared__ uint32_t tmem_at;
+    __shared__ int poison;
     pdl_wait();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tid4 = lane & 3;
-    const int split = blockIdx.x % a.n_split, n0 = blockIdx.x / a.n_split * ROWS, t0 = blockIdx.y * TOK;
-    const int u0 = split * a.units, u1 = min((a.K + LIN_UNIT - 1) / LIN_UNIT, u0 + a.units);
-    const int row_w = 32 * (warp % (ROWS / 32)), tok_w = 32 * (warp / (ROWS / 32));
-    // this thread's chunk of every token row that it brings in, and its row of the codes
-    const int xch = tid & 15;
-    auto load_x = [&](uint4 (&v)[XC], int u) {
-        if (u >= u1) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, h = warp >> 2;
+    const int split = blockIdx.x % a.n_split, n0 = blockIdx.x / a.n_split * TC_ROWS, t0 = blockIdx.y * TOK;
+    const int groups = a.K / G, g0 = split * a.units, n = min(groups, g0 + a.units) - g0;
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "n"(S::COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 0) {
+        mbar_init(&bars[0], 1);
+        mbar_init(&bars[1], 1);
+        poison = 0;
+        fence_barrier_init();
+    }
+    // rows gid and gid + 8 of the 16 that the warp expands, and what the thread brings in of the activations: token tok, chunks
+    // 4 i + tid4 of i in [i0, i0 + TPW)
+    const int gid = lane >> 2, tid4 = lane & 3;
+    const uint8_t* codes[2];
 #pragma unroll
-        for (int i = 0; i < XC; ++i) {
-            const int t = min(t0 + (tid >> 4) + i * (THREADS / 16), a.T - 1), k = u * LIN_UNIT + 8 * xch;
-            v[i] = k < a.K ? __ldg(reinterpret_cast<const uint4*>(a.x + (long long)t * a.K + k)) : make_uint4(0u, 0u, 0u, 0u);
-        }
-    };
-    auto put_x = [&](const uint4 (&v)[XC], Stage& st) {
+    for (int e = 0; e < 2; ++e)
+        codes[e] = a.codes + (long long)min(n0 + 32 * q + 16 * h + gid + 8 * e, a.N - 1) * (a.K / 2) + (long long)g0 * (G / 2) + tid4 * (4 * W);
+    const int oct = warp % S::OCTETS, i0 = warp / S::OCTETS * S::TPW, tok = 8 * oct + gid;
+    const bool brings = warp / S::OCTETS < S::SPLITS;
+    const uint4* xs = reinterpret_cast<const uint4*>(a.x + (long long)min(t0 + tok, a.T - 1) * a.K + (long long)g0 * G) + 4 * i0 + tid4;
+    uint32_t cw[2][2][W];
+    uint4 xv[S::TPW];
+    auto load_codes = [&](uint32_t (&c)[2][W], int i) {
+        if (i >= n) return;
 #pragma unroll
-        for (int i = 0; i < XC; ++i) {
-            uint32_t b[4];
-            b_operands(b, v[i]);
-            st.x[chunk_at<G>((tid >> 4) + i * (THREADS / 16), xch)] = make_uint4(b[0], b[1], b[2], b[3]);
-        }
-    };
-    auto fetch = [&](int u, Stage& st) {   // codes and parameters; rows behind the matrix as its last one
-        if (u < u1) {
-#pragma unroll
-            for (int i = 0; i < ROWS * 4 / THREADS; ++i) {
-                const int c = tid + i * THREADS, row = min(n0 + (c >> 2), a.N - 1), k = u * LIN_UNIT + 32 * (c & 3);
-                if (k < a.K) cp_async16(&st.code[c], a.codes + (long long)row * (a.K / 2) + k / 2);
+        for (int e = 0; e < 2; ++e) {
+            if constexpr (W == 4) {
+                const uint4 v = __ldcs(reinterpret_cast<const uint4*>(codes[e] + i * (G / 2)));
+                c[e][0] = v.x, c[e][1] = v.y, c[e][2] = v.z, c[e][3] = v.w;
+            } else {
+                const uint2 v = __ldcs(reinterpret_cast<const uint2*>(codes[e] + i * (G / 2)));
+                c[e][0] = v.x, c[e][1] = v.y;
             }
+        }
+    };
+    // parameters of groups 8 c .. 8 c + 7: eight lanes a row
+    auto bring_params = [&](int c) {
 #pragma unroll
-            for (int g = 0; g < S::GROUPS; ++g)
-                if (tid < ROWS && u * LIN_UNIT + g * G < a.K)
-                    cp_async4(&st.param[g][tid], a.params + (long long)min(n0 + tid, a.N - 1) * (a.K / G) + u * S::GROUPS + g);
+        for (int u = 0; u < 8 * TC_ROWS / THREADS; ++u) {
+            const int r = (tid >> 3) + u * (THREADS / 8), g = 8 * c + (tid & 7);
+            if (g < n) cp_async4(&params[c & 1][tid & 7][r], a.params + (long long)min(n0 + r, a.N - 1) * groups + g0 + g);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    float acc[2][NT][4];
-    zero(acc[0]);
-    zero(acc[1]);
-    uint4 xv[XC] = {};
-    load_x(xv, u0);
-    fetch(u0, ring[0]);
-    fetch(u0 + 1, ring[1]);
-    put_x(xv, ring[0]);
-    load_x(xv, u0 + 1);
-    int stage = 0;
-    for (int u = u0; u < u1; ++u) {
-        asm volatile("cp.async.wait_group 1;" ::: "memory");   // all but the newest: unit u has landed
-        __syncthreads();                                       // for every thread; the other two stages' readers are through
-        const int next = stage + 1 == LIN_STAGES ? 0 : stage + 1, after = next + 1 == LIN_STAGES ? 0 : next + 1;
-        fetch(u + 2, ring[after]);
-        put_x(xv, ring[next]);
-        load_x(xv, u + 2);
-        const Stage& st = ring[stage];
-        float* sm = &sums[u & 1][0][0];
-        if (warp < TOK / 8) {
+    auto load_x = [&](int i) {
+        if (i >= n || !brings) return;
 #pragma unroll
-            for (int g = 0; g < S::GROUPS; ++g) {
-                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < S::TPW; ++j) xv[j] = __ldg(xs + i * (G / 8) + 4 * j);
+    };
+    bring_params(0);
+    load_codes(cw[0], 0);
+    load_x(0);
+    load_codes(cw[1], 1);
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tm = tmem_at;
+    const uint32_t lanes = (uint32_t)(32 * q) << 16;
+    F2 acc[NC / 2];
 #pragma unroll
-                for (int j = 0; j < S::W; ++j) {
-                    const uint4 v = st.x[chunk_at<G>(8 * warp + gid, g * (G / 8) + S::W * tid4 + j)];
-                    const uint32_t b[4] = {v.x, v.y, v.z, v.w};
-                    sum_mmas(s4, b);
-                }
-                if (gid == 0) *reinterpret_cast<float2*>(sm + g * TOK + 8 * warp + 2 * tid4) = make_float2(s4[0], s4[1]);
+    for (int c = 0; c < NC / 2; ++c) acc[c] = f2(0.f);
+    bool dead = false;
+
+    auto fill = [&](int i, int b) {   // stage i into buffers b; the MMAs that read them last are complete
+        if (brings) {
+            float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < S::TPW; ++j) {
+                mma_bf16(s4, BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, xv[j].x, xv[j].y);
+                mma_bf16(s4, BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, xv[j].z, xv[j].w);
+                // chunk (t, wd): the indices 8 (W t + wd) .. of the group, a lane t's word wd of the codes.  The 16x256b store gives
+                // the lane's pairs 2 j, 2 j + 1 the columns 8 j + 2 t, + 1, half t & 1 of the octet 2 j + (t >> 1).
+                uint32_t p[4];
+                b_operands(p, xv[j]);
+                const int c = 4 * (i0 + j) + tid4, t = c / W, wd = c % W;
+                const uint32_t at = smem_u32(smem) + b * S::XBUF + (4 * wd + (t >> 1)) * S::LBO + tok * 16 + 8 * (t & 1);
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(p[0]), "r"(p[1]) : "memory");
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + 2 * S::LBO), "r"(p[2]), "r"(p[3]) : "memory");
             }
+            if (lane < 4) *reinterpret_cast<float2*>(&sums[i % 3][warp / S::OCTETS][8 * oct + 2 * lane]) = make_float2(s4[0], s4[1]);
         }
+        load_x(i + 1);
+        uint32_t r[8 * W];
 #pragma unroll
-        for (int g = 0; g < S::GROUPS; ++g) {
-            if (g && u * LIN_UNIT + g * G >= a.K) break;
-            float c[2][NT][4];
-            uint32_t cw[2][2][S::W];
+        for (int j = 0; j < 2 * W; ++j)
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                zero(c[r]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4* p = &st.code[(row_w + 16 * r + 8 * h + gid) * 4];
-                    if constexpr (S::GROUPS == 1) {
-                        const uint4 v = p[tid4];
-                        cw[r][h][0] = v.x, cw[r][h][1] = v.y, cw[r][h][2] = v.z, cw[r][h][3] = v.w;
-                    } else {
-                        const uint2 v = reinterpret_cast<const uint2*>(p)[4 * g + tid4];
-                        cw[r][h][0] = v.x, cw[r][h][1] = v.y;
-                    }
-                }
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t w = cw[b][e][j >> 1];
+                r[4 * j + 2 * e] = j & 1 ? code_pair<2>(w, a.bits) : code_pair<0>(w, a.bits);
+                r[4 * j + 2 * e + 1] = j & 1 ? code_pair<3>(w, a.bits) : code_pair<1>(w, a.bits);
             }
+        if constexpr (W == 4) tc_st_x8(tm + ((uint32_t)(32 * q + 16 * h) << 16) + b * S::A_COLS, r);
+        else tc_st_x4(tm + ((uint32_t)(32 * q + 16 * h) << 16) + b * S::A_COLS, r);
+        load_codes(cw[b], i + 2);
+        tc_wait_st();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the activations' stores, before the MMAs read them
+        tc_fence_before();
+    };
+    auto issue = [&](int b) {
+        tc_fence_after();
+        const uint64_t bd = tc_desc(smem_u32(smem) + b * S::XBUF, S::LBO, 128);
+        constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TOK / 8) << 17) | ((128u / 16) << 24);
+        linear_mmas<G, 2 * S::LBO / 16>(__shfl_sync(0xffffffffu, tm + 2 * S::A_COLS + b * TOK, 0), __shfl_sync(0xffffffffu, tm + b * S::A_COLS, 0),
+                                        bd, idesc, smem_u32(&bars[b]));
+    };
+    auto fold = [&](int i, int b) {
+        if (!dead) dead = !warp_wait(smem_u32(&bars[b]), (i >> 1) & 1, &poison, g_linear_status, 1, i);
+        tc_fence_after();
+        const uint32_t from = tm + lanes + 2 * S::A_COLS + b * TOK + h * NC;
+        uint32_t r[NC];
 #pragma unroll
-            for (int j = 0; j < S::W; ++j) {
-                uint32_t b[NT][4];
+        for (int c = 0; c < NC; c += 8) tc_ld_rows8(from + c, r + c);
+        const uint32_t pw = params[(i >> 3) & 1][i & 7][32 * q + lane];
+        const __half2 pv = *reinterpret_cast<const __half2*>(&pw);
+        const float s1 = __low2float(pv);
+        const F2 s2 = f2(s1), m2 = f2(fmaf(-16.f, s1, __high2float(pv)));
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint4 v = st.x[chunk_at<G>(tok_w + 8 * n + gid, g * (G / 8) + S::W * tid4 + j)];
-                    b[n][0] = v.x, b[n][1] = v.y, b[n][2] = v.z, b[n][3] = v.w;
-                }
+        for (int c = 0; c < NC; c += 4)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) word_mmas(c[r], cw[r][0][j], cw[r][1][j], a.bits, b);
+            for (int sp = 0; sp < S::SPLITS; ++sp) {
+                const float4 v = *reinterpret_cast<const float4*>(&sums[i % 3][sp][h * NC + c]);
+                acc[c / 2] = fma2(m2, f2(v.x, v.y), acc[c / 2]);
+                acc[c / 2 + 1] = fma2(m2, f2(v.z, v.w), acc[c / 2 + 1]);
             }
-            if (g == 0) __syncthreads();   // the sums are there
-            float sx[NT][2];
+        tc_wait_ld();
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float2 v = *reinterpret_cast<const float2*>(sm + g * TOK + tok_w + 8 * n + 2 * tid4);
-                sx[n][0] = v.x, sx[n][1] = v.y;
+        for (int c = 0; c < NC; c += 8)   // (what is read of them stays behind the wait)
+            asm volatile("" : "+r"(r[c]), "+r"(r[c + 1]), "+r"(r[c + 2]), "+r"(r[c + 3]), "+r"(r[c + 4]), "+r"(r[c + 5]), "+r"(r[c + 6]), "+r"(r[c + 7]));
+#pragma unroll
+        for (int c = 0; c < NC; c += 2) acc[c / 2] = fma2(s2, f2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), acc[c / 2]);
+        tc_fence_before();
+    };
+    fill(0, 0);
+    __syncthreads();
+    if (warp == 0) issue(0);
+    for (int i = 0; i < n; i += 2) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (i + b >= n) break;
+            // the next eight groups' parameters: asked for at the second stage of eight (every warp has folded the eight before, whose
+            // place they take), there at the last
+            if (((i + b) & 7) == 1 && (((i + b) >> 3) + 1) * 8 < n) bring_params(((i + b) >> 3) + 1);
+            if (i + b + 1 < n) {
+                fill(i + b + 1, b ^ 1);
+                if (((i + b) & 7) == 7) asm volatile("cp.async.wait_group 0;" ::: "memory");
+                __syncthreads();   // stage i + b + 1 is filled, stage i + b - 1 folded by every warp
+                if (warp == 0) issue(b ^ 1);
             }
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                fold_group(acc[r], c[r], sx, st.param[g][row_w + 16 * r + gid], st.param[g][row_w + 16 * r + 8 + gid]);
+            fold(i + b, b);
         }
-        stage = next;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(S::COLS) : "memory");
     }
     // results to shared memory, [token][row], then out in whole rows of a token
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();
+    const bool bad = *(volatile int*)&poison;
     float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                part[(tok_w + 8 * n + 2 * tid4 + (i & 1)) * ROWS + row_w + 16 * r + gid + 8 * (i >> 1)] = acc[r][n][i];
+    for (int c = 0; c < NC; ++c)
+        part[(h * NC + c) * TC_ROWS + 32 * q + lane] = bad ? __int_as_float(0x7fffffff) : (c & 1 ? hi(acc[c / 2]) : lo(acc[c / 2]));
     if (a.n_split == 1) {
         __syncthreads();
-        for (int o = tid; o < TOK * ROWS; o += THREADS) store_y<TO>(a, t0 + o / ROWS, n0 + o % ROWS, part[o]);
+        for (int o = tid; o < TOK * TC_ROWS; o += THREADS) store_y<TO>(a, t0 + o / TC_ROWS, n0 + o % TC_ROWS, part[o]);
         return;
     }
     cluster_sync_all();
-    for (int o = split * THREADS + tid; o < TOK * ROWS; o += a.n_split * THREADS)
-        store_y<TO>(a, t0 + o / ROWS, n0 + o % ROWS, cluster_sum(part, o, a.n_split));
+    for (int o = split * THREADS + tid; o < TOK * TC_ROWS; o += a.n_split * THREADS)
+        store_y<TO>(a, t0 + o / TC_ROWS, n0 + o % TC_ROWS, cluster_sum(part, o, a.n_split));
     cluster_sync_all();
 }
 
 // Shares of the input indices, a CTA of a cluster each: as many as leave the fewest units to the SM with most work.
-static void split_units(LinearArgs& a, long long blocks, int n_sms, int per_sm, int least) {
-    const int units = (a.K + LIN_UNIT - 1) / LIN_UNIT;
+#ifndef LIN_OVER
+#define LIN_OVER 12
+#endif
+#ifndef LIN_FEW
+#define LIN_FEW 16
+#endif
+static void split_units(LinearArgs& a, int units, long long blocks, int n_sms, int per_sm, int least, int start) {
     int best = 1;
     double best_cost = 1e30;
     for (int c = 1; c <= LIN_MAX_CLUSTER; ++c) {
         const int share = (units + c - 1) / c;
         if (c > 1 && share < least) break;
         const long long rounds = (blocks * c + (long long)n_sms * per_sm - 1) / ((long long)n_sms * per_sm);
-        const double cost = (double)rounds * (share + 12);
+        const double cost = (double)rounds * (share + start);
         if (cost < 0.95 * best_cost) best = c, best_cost = cost;
     }
     const int share = (units + best - 1) / best;
@@ -485,31 +573,27 @@ static void split_units(LinearArgs& a, long long blocks, int n_sms, int per_sm, 
 template <int NT, int R, int U, int G>
 static cudaError_t linear_few(LinearArgs a, int y_f32, int n_sms, cudaStream_t st) {
     const unsigned blocks = (unsigned)((a.N + 16 * R - 1) / (16 * R)), tiles = (unsigned)((a.T + 8 * NT - 1) / (8 * NT));
-    split_units(a, (long long)blocks * tiles, n_sms, 2, LIN_WARPS);
+    split_units(a, (a.K + LIN_UNIT - 1) / LIN_UNIT, (long long)blocks * tiles, n_sms, 2, LIN_WARPS, 12);
     const dim3 grid(blocks * a.n_split, tiles);
     return y_f32 ? launch_pdl_cluster(linear_few_kernel<NT, R, U, G, float>, grid, dim3(32 * LIN_WARPS), 0, a.n_split, st, a)
                  : launch_pdl_cluster(linear_few_kernel<NT, R, U, G, __nv_bfloat16>, grid, dim3(32 * LIN_WARPS), 0, a.n_split, st, a);
 }
 template <int TOK, int G>
-static cudaError_t linear_tile(LinearArgs a, int y_f32, int n_sms, cudaStream_t st) {
-    constexpr int ROWS = TileStage<G, TOK>::ROWS;
-    constexpr int SMEM = LIN_STAGES * (int)sizeof(TileStage<G, TOK>);
-    static_assert(SMEM >= TOK * ROWS * 4, "the results go where the stages were");
-    const unsigned blocks = (unsigned)((a.N + ROWS - 1) / ROWS), tiles = (unsigned)((a.T + TOK - 1) / TOK);
-    split_units(a, (long long)blocks * tiles, n_sms, 2, 4);
+static cudaError_t linear_tc(LinearArgs a, int y_f32, int n_sms, cudaStream_t st) {
+    constexpr int SMEM = TcShape<TOK, G>::SMEM;
+    const unsigned blocks = (unsigned)((a.N + TC_ROWS - 1) / TC_ROWS), tiles = (unsigned)((a.T + TOK - 1) / TOK);
+    split_units(a, a.K / G, (long long)blocks * tiles, n_sms, 2, 4, LIN_OVER);
     const dim3 grid(blocks * a.n_split, tiles);
-    auto go = [&](auto kernel) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-        return e != cudaSuccess ? e : launch_pdl_cluster(kernel, grid, dim3(32 * LIN_WARPS), SMEM, a.n_split, st, a);
-    };
-    return y_f32 ? go(linear_tile_kernel<TOK, G, float>) : go(linear_tile_kernel<TOK, G, __nv_bfloat16>);
+    auto go = [&](auto kernel) { return launch_pdl_cluster(kernel, grid, dim3(32 * LIN_WARPS), SMEM, a.n_split, st, a); };
+    return y_f32 ? go(linear_tc_kernel<TOK, G, float>) : go(linear_tc_kernel<TOK, G, __nv_bfloat16>);
 }
 template <int G>
 static cudaError_t linear_by_tokens(const LinearArgs& a, int y_f32, int n_sms, cudaStream_t st) {
-    if (a.T <= 8) return a.N >= 64 * n_sms ? linear_few<1, 2, 2, G>(a, y_f32, n_sms, st) : linear_few<1, 1, 4, G>(a, y_f32, n_sms, st);
-    if (a.T <= 16) return linear_few<2, 2, 2, G>(a, y_f32, n_sms, st);
-    if (a.T <= 32) return linear_tile<32, G>(a, y_f32, n_sms, st);
-    return linear_tile<64, G>(a, y_f32, n_sms, st);
+    if (a.T <= LIN_FEW && a.T <= 8) return a.N >= 64 * n_sms ? linear_few<1, 2, 2, G>(a, y_f32, n_sms, st) : linear_few<1, 1, 4, G>(a, y_f32, n_sms, st);
+    if (a.T <= LIN_FEW) return linear_few<2, 2, 2, G>(a, y_f32, n_sms, st);
+    if (a.T <= 16) return linear_tc<16, G>(a, y_f32, n_sms, st);
+    if (a.T <= 32) return linear_tc<32, G>(a, y_f32, n_sms, st);
+    return linear_tc<64, G>(a, y_f32, n_sms, st);
 }
 
 }  // namespace dyn
@@ -539,6 +623,16 @@ dynamo_status dynamo_linear_quantize(const void* w, int32_t rows, int32_t cols, 
                       (const __nv_bfloat16*)w, n, group_size, (uint8_t*)codes, (__half2*)params) == cudaSuccess
                ? DYNAMO_OK
                : DYNAMO_ERR_CUDA;
+}
+
+dynamo_status dynamo_linear_poll_status(void* stream) {
+    if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return DYNAMO_ERR_CUDA;
+    int32_t word = 0;
+    if (cudaMemcpyFromSymbol(&word, g_linear_status, 4) != cudaSuccess) return DYNAMO_ERR_CUDA;
+    if (word == 0) return DYNAMO_OK;
+    const int32_t zero[16] = {};
+    if (cudaMemcpyToSymbol(g_linear_status, zero, sizeof(zero)) != cudaSuccess) return DYNAMO_ERR_CUDA;
+    return DYNAMO_ERR_TIMEOUT;
 }
 
 dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size, const void* codes,
