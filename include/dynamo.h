@@ -453,17 +453,21 @@ dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void
  * dynamo_linear_quantize: w bf16 [rows, cols] -> codes uint8 [rows, cols / 2] (index 2i in the low, 2i + 1 in the high half of
  *   byte i) and params fp16 [rows, cols / G, 2] {scale, zero}, by the rule of dynamo_pack_experts at 4 bits.
  * dynamo_linear_forward: y[t][n] = sum_k (scale[n][k/G] * code[n][k] + zero[n][k/G]) * x[t][k]
- *   x bf16 [T, cols], y [T, rows] of y_dtype.  Products are exact, sums in fp32.  Made for the few rows of a decode step; the
- *   matrix is read once per 32 tokens at most.  An infinite or NaN activation makes its row NaN; the sum of 31 |x| over a group
+ *   x bf16 [T, cols], y [T, rows] of y_dtype.  Products are exact, sums in fp32.  Made for the few rows of a decode step:
+ *   large matrices are read once per 64 tokens, small ones (16 tokens x the matrix up to 3 * 2^24) per 16.  An infinite or NaN activation makes its row NaN; the sum of 31 |x| over a group
  *   has to stay in the range of fp32.
+ *   workspace: dynamo_linear_workspace_bytes (0 for up to 8 tokens and small matrices: then it may be NULL), 256-byte aligned.
  * dynamo_linear_poll_status: synchronises the stream; DYNAMO_ERR_TIMEOUT if a bounded wait of dynamo_linear_forward expired on the
  *   current device since the last call (the results concerned are NaN), else DYNAMO_OK.
- * group_size 64 or 128, cols a multiple of it up to 2^24, rows >= 1 (ERR_SHAPE); 0 <= T <= DYNAMO_LINEAR_MAX_TOKENS (ERR_TOKENS). */
+ * group_size 64 or 128, cols a multiple of it, both up to 2^24, rows >= 1 (ERR_SHAPE); 0 <= T <= DYNAMO_LINEAR_MAX_TOKENS, and
+ *   T * rows * cols below 2^50 or so (ERR_TOKENS). */
 #define DYNAMO_LINEAR_MAX_TOKENS 65536
 dynamo_status dynamo_linear_quantize(const void* w, int32_t rows, int32_t cols, int32_t group_size, void* codes, void* params,
                                      void* stream);
 dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size,
-                                    const void* codes, const void* params, void* y, int32_t y_dtype, void* stream);
+                                    const void* codes, const void* params, void* y, int32_t y_dtype,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+dynamo_status dynamo_linear_workspace_bytes(int32_t T, int32_t rows, int32_t cols, int32_t group_size, size_t* bytes);
 dynamo_status dynamo_linear_poll_status(void* stream);
 
 #ifdef __cplusplus

@@ -41,7 +41,8 @@ EXPORTED = ["dynamo_create", "dynamo_destroy", "dynamo_arena_bytes", "dynamo_pac
             "dynamo_debug_expire_wait", "dynamo_debug_check_guards",
             "dynamo_dispatch_workspace_bytes", "dynamo_dispatch", "dynamo_combine", "dynamo_combine_backward",
             "dynamo_norm_join_forward", "dynamo_norm_join_workspace_bytes", "dynamo_norm_join_backward",
-            "dynamo_linear_quantize", "dynamo_linear_forward", "dynamo_linear_poll_status",
+            "dynamo_linear_quantize", "dynamo_linear_forward", "dynamo_linear_workspace_bytes",
+            "dynamo_linear_poll_status",
             "dynamo_kernel_launches", "dynamo_status_str"]
 
 
@@ -118,7 +119,8 @@ def load():
         L.dynamo_norm_join_workspace_bytes.argtypes = [jd, i32, ctypes.POINTER(sz)]
         L.dynamo_norm_join_backward.argtypes = [jd, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.dynamo_linear_quantize.argtypes = [vp, i32, i32, i32, vp, vp, vp]
-        L.dynamo_linear_forward.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp]
+        L.dynamo_linear_forward.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp, sz, vp]
+        L.dynamo_linear_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.dynamo_linear_poll_status.argtypes = [vp]
         L.dynamo_kernel_launches.argtypes = [vp]
         L.dynamo_kernel_launches.restype = ctypes.c_int64

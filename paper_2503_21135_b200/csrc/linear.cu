@@ -9,6 +9,7 @@
 // bf16); sums, scales and zero-points are in fp32, y is rounded once.  The order in which a warp's 16-wide steps take the
 // input indices is free as long as codes and activations agree: a lane takes runs of consecutive ones from both.
 #include <algorithm>
+#include <cstddef>
 #include <type_traits>
 
 #include "../../include/dynamo.h"
@@ -77,6 +78,8 @@ struct LinearArgs {
     void* y;                  // [T, N]
     int T, K, N;
     PairBits bits;
+    const uint8_t* xt;        // tcgen05 kernel: activations in its order
+    float* part;              // and partial results, two tiles a CTA
     int n_split, units;       // shares of the input indices (CTAs of a cluster), units of LIN_UNIT in a share
 };
 
@@ -206,7 +209,7 @@ __device__ __forceinline__ float cluster_sum(const float* part, int i, int n_cta
     return s;
 }
 
-// ---- few tokens (up to 16): bound by the codes ----------------------------------------------------------------------------
+// ---- few tokens, small matrices: bound by the codes ----------------------------------------------------------------------------
 // CTA: 16 R rows, 8 NT tokens, of a cluster's CTAs along the input indices the blockIdx.x % n_split-th share; its warps take the
 // share's units in turn, U units' codes on their way to a warp at any time, and add up their sums at the end.
 template <int NT, int R, int U, int G, typename TO>
@@ -298,263 +301,488 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 }
 
 // ---- tcgen05: the codes as the A operand in tensor memory -------------------------------------------------------------------
-// CTA: 128 rows, TOK tokens, a share of the groups; eight warps that all do the same.  Warp w has the lane quarter q = w % 4 of the
-// tensor memory: rows 32 q .., of which it expands 16 and folds all, half of the tokens (h = w / 4 says which).
-// A stage is one group:
-//   fill    codes of 16 rows -> 16 + q as bf16 pairs -> tensor memory (A, G / 2 columns; 16x256b, so that four lanes read a row's codes:
-//           a row a lane kept the L1 busy with 32 lines a load); the activations -> shared memory (B, K-major core matrices of 8 tokens x
-//           8 indices), in the order that this gives the indices, their sums by an mma.sync whose other operand is ones, from the
-//           registers that they came in; parameters of eight groups at a time -> shared memory
-//   MMAs    G / 16 tcgen05.mma of 128 x TOK x 16 into one of two accumulators, issued by one warp in one run, committed to a barrier
-//   fold    y += s * acc + (m - 16 s) * sum(x), two columns an instruction
-// Stage i + 1 is filled and its MMAs issued before stage i is folded: one barrier a stage, and the MMAs run under the next
-// stage's filling.  Two CTAs share an SM (each 256 columns of tensor memory at most, 128 registers a thread).
-// A poll of the MMAs' barrier is bounded; after an expired one the CTA's outputs are NaN and the status word is set.  The tensor
-// memory is given back before the CTAs of a cluster meet: nobody waits for another CTA while it holds some.
-constexpr int TC_ROWS = 128;
+// The work is a line of stages: 256 rows (two row tiles of an MMA's 128) x 128 input indices for TOK tokens, a block's stages one behind
+// another; one persistent CTA per SM takes an equal run of it.  Roles by warp:
+//   0-7   expand : two groups of four (a warp per lane quarter of the tensor memory); a group takes every other stage: 16 rows x 128
+//                  indices of codes at a time -> 16 + q as bf16 pairs -> A buffer (16x256b stores, so that four lanes read a
+//                  row's codes; a row a lane kept the L1 busy with 32 lines a load).  The codes come by cp.async, three jobs of a warp
+//                  on their way: 96 KB an SM (one job in registers left the loads' latency to bind)
+//   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + (m - 16 s) * sum(x), two columns an instruction;
+//                  sixteen warps at 64 tokens, half of the columns each: eight took 84 us where sixteen take less than the expansion
+//   next  fetch  : one thread; a bulk copy a stage of the activations, which linear_x_kernel has put into the operand's order,
+//                  with their sums per group behind them
+//   last  MMA    : 2 * 128 / 16 tcgen05.mma of 128 x TOK x 16 a stage, a run and one commit
+// Roles meet at barriers only, so that the chain of a stage (codes, expansion, MMAs, fold) overlaps its neighbours', blocks' ends
+// included; the same work by eight warps that all did every part, a barrier of the CTA a stage, took 88 us at 64 tokens, 14336 x 14336.
+// A block that lies within one CTA's run goes from the fold warps' registers to y; the pieces of the others go to the workspace, and a
+// kernel behind this one adds them up in the order of the CTAs.
+// Tensor memory: two A buffers of 128 columns, then BUFS accumulator buffers of 2 * TOK, one a group.
+// Every wait is bounded; after an expired one the roles end, the CTA's remaining results are NaN and the status word is set.
+constexpr int TC_ROWS = 256;
+constexpr int TC_SLOTS = 4;       // stages of activations on their way or in use
+constexpr int TC_JOBS = 3;        // jobs (four atoms of a stage) of an expand warp whose codes are on their way or in use
+constexpr int TC_COLS = 512;
+constexpr int TC_MAX_CTAS = 160;  // that the workspace has room for
 static __device__ int32_t g_linear_status[16];
 
 template <int TOK, int G>
 struct TcShape {
-    static constexpr int OCTETS = TOK / 8, QUADS = G / 32;                       // eight tokens, 32 indices: a warp's task of the filling
-    static constexpr int TPW = OCTETS * QUADS < LIN_WARPS ? 1 : OCTETS * QUADS / LIN_WARPS;
-    static constexpr int SPLITS = QUADS / TPW;                                   // warps that share an octet: partial sums
-    static constexpr int LBO = TOK * 16 + 16;   // bytes between octets of indices; the pad keeps the filling's stores off one another's banks
-    static constexpr int XBUF = G / 8 * LBO;
-    static constexpr int W = G / 32;                                             // words of codes of a lane and row: a quarter of a group
-    static constexpr int A_COLS = G / 2, COLS = 2 * A_COLS + 2 * TOK <= 64 ? 64 : 2 * A_COLS + 2 * TOK <= 128 ? 128 : 256;
-    static constexpr int SMEM = 2 * XBUF > TOK * TC_ROWS * 4 ? 2 * XBUF : TOK * TC_ROWS * 4;
-    static_assert(2 * A_COLS + 2 * TOK <= COLS, "tensor memory");
+    static constexpr int GROUPS = LIN_UNIT / G, W = G / 32;     // groups of a stage; words of codes of a lane, row and group
+    static constexpr int LBO = TOK * 16;                        // bytes between octets of indices
+    static constexpr int XB = 16 * LBO + GROUPS * TOK * 4;      // bytes of a stage's activations and sums
+    static constexpr int BUFS = TOK == 64 ? 2 : 4;
+    static constexpr int FOLDS = TOK == 64 ? 16 : 8;             // fold warps: (lane quarter, row tile), and half of the tokens where there are 64
+    static constexpr int NC = TOK * 8 / FOLDS;                  // columns of a fold warp
+    static constexpr int W_FETCH = 8 + FOLDS, W_MMA = W_FETCH + 1, WARPS = W_MMA + 1;
+    static constexpr int CODES = 8 * TC_JOBS * 4096;            // bytes of the expand warps' rings
+    static constexpr int SMEM = CODES + TC_SLOTS * XB;
+    static_assert(256 + BUFS * 2 * TOK <= TC_COLS, "tensor memory");
+    static_assert(XB % 16 == 0, "bulk copies");
 };
 
-// The MMAs of a stage: G / 16 steps of 16 indices, A columns 8 k, B octets 2 k.  The first starts from zero.
-#define LIN_MMA(k, acc)                                                  \
-    "add.s64 bd, %2, " #k "*%4;\n\tadd.s32 aa, %1, " #k "*8;\n\t"        \
-    "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [aa], bd, %3, " acc ";\n\t"
-template <int G, int STEP>
-__device__ __forceinline__ void linear_mmas(uint32_t d, uint32_t a, uint64_t bd, uint32_t idesc, uint32_t bar) {
-    if constexpr (G == 128)
-        asm volatile(
-            "{\n\t.reg .pred q, p0, p1;\n\t.reg .b64 bd;\n\t.reg .b32 aa;\n\telect.sync _|q, 0xffffffff;\n\t"
-            "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t" LIN_MMA(0, "p0") LIN_MMA(1, "p1") LIN_MMA(2, "p1") LIN_MMA(3, "p1")
-                LIN_MMA(4, "p1") LIN_MMA(5, "p1") LIN_MMA(6, "p1") LIN_MMA(7, "p1")
-            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d), "r"(a), "l"(bd), "r"(idesc),
-            "n"(STEP), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred q, p0, p1;\n\t.reg .b64 bd;\n\t.reg .b32 aa;\n\telect.sync _|q, 0xffffffff;\n\t"
-            "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t" LIN_MMA(0, "p0") LIN_MMA(1, "p1") LIN_MMA(2, "p1") LIN_MMA(3, "p1")
-            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d), "r"(a), "l"(bd), "r"(idesc),
-            "n"(STEP), "r"(bar)
-            : "memory");
-}
-__device__ __forceinline__ void cp_async4(void* dst, const void* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-}
-// Eight consecutive columns of the warp's 32 lanes, a row a lane.
-__device__ __forceinline__ void tc_ld_rows8(uint32_t at, uint32_t* r) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(at)
-                 : "memory");
+// Activations in the order of the B operand, K-major core matrices of 8 tokens x 8 indices: [token tile][stage][octet of indices 16]
+// [token TOK][16 bytes], then the sums [group][TOK].  A warp has eight tokens of a stage.  Chunk (t, wd) of a group, the indices
+// 8 (W t + wd) .., is a lane t's word wd of the codes; the 16x256b store gives the word's pairs 2 j, 2 j + 1 (j counted over
+// the lane's words) the columns 8 j + 2 t, + 1: half t & 1 of octet 2 j + (t >> 1).  The sums come from MMAs with ones.
+template <int TOK, int G>
+__global__ void __launch_bounds__(256) linear_x_kernel(const __nv_bfloat16* __restrict__ x, int T, int K, int stages, int tiles,
+                                                       uint8_t* __restrict__ out) {
+    using S = TcShape<TOK, G>;
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, gid = lane >> 2, tid4 = lane & 3;
+    const int w = blockIdx.x * 8 + (threadIdx.x >> 5), stage = w % stages, oct = w / stages;   // octets of tokens over all tiles
+    if (oct >= tiles * (TOK / 8)) return;
+    const int tile = oct / (TOK / 8), tok = 8 * (oct % (TOK / 8)) + gid;
+    const __nv_bfloat16* row = x + (long long)min(TOK * tile + tok, T - 1) * K + (long long)stage * LIN_UNIT;
+    uint8_t* to = out + ((long long)tile * stages + stage) * S::XB;
+    uint4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = 4 * i + tid4;
+        v[i] = stage * LIN_UNIT + 8 * c < K ? *reinterpret_cast<const uint4*>(row + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    float sum[S::GROUPS][4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        mma_bf16(sum[i * S::GROUPS / 4], BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, v[i].x, v[i].y);
+        mma_bf16(sum[i * S::GROUPS / 4], BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, v[i].z, v[i].w);
+        uint32_t p[4];
+        b_operands(p, v[i]);
+        const int c = 4 * i + tid4, g = c / (4 * S::W), t = c % (4 * S::W) / S::W, wd = c % S::W;
+        uint8_t* at = to + (G / 8 * g + 4 * wd + (t >> 1)) * S::LBO + tok * 16 + 8 * (t & 1);
+        *reinterpret_cast<uint2*>(at) = make_uint2(p[0], p[1]);
+        *reinterpret_cast<uint2*>(at + 2 * S::LBO) = make_uint2(p[2], p[3]);
+    }
+    if (lane < 4)
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g)
+            *reinterpret_cast<float2*>(to + 16 * S::LBO + (g * TOK + 8 * (oct % (TOK / 8)) + 2 * lane) * 4) = make_float2(sum[g][0], sum[g][1]);
 }
 
-template <int TOK, int G, typename TO>
-__global__ void __launch_bounds__(32 * LIN_WARPS, 2) linear_tc_kernel(const __grid_constant__ LinearArgs a) {
-    using S = TcShape<TOK, G>;
-    constexpr int THREADS = 32 * LIN_WARPS, NC = TOK / 2, W = S::W;   // NC: columns that a warp folds
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(16) float sums[3][S::SPLITS][TOK];
-    __shared__ uint32_t params[2][8][TC_ROWS];   // of eight groups, and of the next eight
-    __shared__ uint64_t bars[2];
-    __shared__ uint32_t tmem_at;
-    __shared__ int poison;
-    pdl_wait();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, h = warp >> 2;
-    const int split = blockIdx.x % a.n_split, n0 = blockIdx.x / a.n_split * TC_ROWS, t0 = blockIdx.y * TOK;
-    const int groups = a.K / G, g0 = split * a.units, n = min(groups, g0 + a.units) - g0;
-    if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "n"(S::COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+struct TcShared {
+    uint64_t x_full[TC_SLOTS], x_empty[TC_SLOTS];   // a stage's activations have landed; the fold warps are done with the stage
+    uint64_t a_full[2], a_empty[2];                 // the four expand warps of the stage have stored it; its MMAs are complete
+    uint64_t acc_full[4], acc_empty[4];             // a group's MMAs are complete; the fold warps have read the accumulator buffer
+    uint32_t tmem;
+    volatile int poison;
+};
+struct TcRole {
+    TcShared* S;
+    uint32_t sb, ring, codes, tm;   // shared-memory addresses of the barriers, the activations and the codes; tensor memory
+    int stages, blocks;             // stages of a block, blocks of a token tile
+    int first, n;                   // the CTA's run: first stage (over all blocks and token tiles) and length
+};
+#define TC_BAR(field, i) (R.sb + (uint32_t)offsetof(TcShared, field) + 8u * (uint32_t)(i))
+
+// Where a role is in the line of stages: token tile, first row, stage of the block.
+struct TcPos {
+    int tile, n0, u;
+    __device__ __forceinline__ TcPos(const TcRole& R) {
+        const int block = R.first / R.stages;
+        u = R.first - block * R.stages;
+        tile = block / R.blocks;
+        n0 = (block - tile * R.blocks) * TC_ROWS;
     }
-    if (tid == 0) {
-        mbar_init(&bars[0], 1);
-        mbar_init(&bars[1], 1);
-        poison = 0;
-        fence_barrier_init();
+    __device__ __forceinline__ bool step(const TcRole& R) {   // true: to another block
+        if (++u < R.stages) return false;
+        u = 0;
+        n0 += TC_ROWS;
+        if (n0 == R.blocks * TC_ROWS) n0 = 0, ++tile;
+        return true;
     }
-    // rows gid and gid + 8 of the 16 that the warp expands, and what the thread brings in of the activations: token tok, chunks
-    // 4 i + tid4 of i in [i0, i0 + TPW)
-    const int gid = lane >> 2, tid4 = lane & 3;
-    const uint8_t* codes[2];
+};
+// CTA c of n: the stages [c U / n, (c + 1) U / n) of U.
+__host__ __device__ __forceinline__ int tc_first(int c, int n, int U) { return (int)((long long)c * U / n); }
+
+// Groups that stage u has (the last may have one of two).
+template <int G>
+__device__ __forceinline__ int stage_groups(int u, int K) {
+    return G == LIN_UNIT ? 1 : min(LIN_UNIT / G, K / G - u * (LIN_UNIT / G));
+}
+
+template <int G>
+__device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int warp, int lane) {
+    using S = TcShape<64, G>;
+    const int q = warp & 3, kh = warp >> 2, gid = lane >> 2, tid4 = lane & 3;
+    // (copies: behind every asm that may write memory the arguments would be read again)
+    const PairBits bits = a.bits;
+    const int N = a.N, K = a.K;
+    TcShared* const sh = R.S;
+    const uint8_t* const base = a.codes;
+    const uint32_t mine = R.codes + warp * (TC_JOBS * 4096) + lane * 16;   // [job][atom][row half][lane] 16 bytes
+    TcPos ahead(R);
+    if (kh) ahead.step(R);
+    int s_ahead = kh;
+    uint32_t rows[4][2];   // byte offsets of the lane's rows 128 (i >> 1) + 32 q + 16 (i & 1) + gid (+ 8) in the block
+    const uint8_t* from;   // of the block's first row, at the lane's place
+    auto block_ahead = [&]() {
+        from = base + (long long)ahead.n0 * (K / 2) + tid4 * (4 * S::W);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-        codes[e] = a.codes + (long long)min(n0 + 32 * q + 16 * h + gid + 8 * e, a.N - 1) * (a.K / 2) + (long long)g0 * (G / 2) + tid4 * (4 * W);
-    const int oct = warp % S::OCTETS, i0 = warp / S::OCTETS * S::TPW, tok = 8 * oct + gid;
-    const bool brings = warp / S::OCTETS < S::SPLITS;
-    const uint4* xs = reinterpret_cast<const uint4*>(a.x + (long long)min(t0 + tok, a.T - 1) * a.K + (long long)g0 * G) + 4 * i0 + tid4;
-    uint32_t cw[2][2][W];
-    uint4 xv[S::TPW];
-    auto load_codes = [&](uint32_t (&c)[2][W], int i) {
-        if (i >= n) return;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if constexpr (W == 4) {
-                const uint4 v = __ldcs(reinterpret_cast<const uint4*>(codes[e] + i * (G / 2)));
-                c[e][0] = v.x, c[e][1] = v.y, c[e][2] = v.z, c[e][3] = v.w;
-            } else {
-                const uint2 v = __ldcs(reinterpret_cast<const uint2*>(codes[e] + i * (G / 2)));
-                c[e][0] = v.x, c[e][1] = v.y;
-            }
-        }
+            for (int e = 0; e < 2; ++e)
+                rows[i][e] = (uint32_t)min(128 * (i >> 1) + 32 * q + 16 * (i & 1) + gid + 8 * e, N - 1 - ahead.n0) * (uint32_t)(K / 2);
     };
-    // parameters of groups 8 c .. 8 c + 7: eight lanes a row
-    auto bring_params = [&](int c) {
+    block_ahead();
+    auto bring = [&](int job) {   // the four atoms of the next stage
+        if (s_ahead < R.n) {
+            const uint32_t k = (uint32_t)ahead.u * (LIN_UNIT / 2);
+            const int ng = stage_groups<G>(ahead.u, K);
 #pragma unroll
-        for (int u = 0; u < 8 * TC_ROWS / THREADS; ++u) {
-            const int r = (tid >> 3) + u * (THREADS / 8), g = 8 * c + (tid & 7);
-            if (g < n) cp_async4(&params[c & 1][tid & 7][r], a.params + (long long)min(n0 + r, a.N - 1) * groups + g0 + g);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint8_t* at = from + (rows[i][e] + k);
+                    const uint32_t to = mine + job * 4096 + i * 1024 + e * 512;
+                    if constexpr (G == LIN_UNIT) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at) : "memory");
+                    } else {   // eight bytes of either group
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(at) : "memory");
+                        if (ng == 2) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + 8), "l"(at + G / 2) : "memory");
+                    }
+                }
+            s_ahead += 2;
+            const bool a1 = ahead.step(R), a2 = ahead.step(R);
+            if (a1 || a2) block_ahead();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto load_x = [&](int i) {
-        if (i >= n || !brings) return;
 #pragma unroll
-        for (int j = 0; j < S::TPW; ++j) xv[j] = __ldg(xs + i * (G / 8) + 4 * j);
-    };
-    bring_params(0);
-    load_codes(cw[0], 0);
-    load_x(0);
-    load_codes(cw[1], 1);
+    for (int j = 0; j < TC_JOBS; ++j) bring(j);
+    int job = 0;
+    uint32_t par = 1;   // of the round that emptied the A buffer before (passes at once the first time)
+    for (int s = kh; s < R.n; s += 2, par ^= 1) {
+        const uint32_t free = bar_test(TC_BAR(a_empty, kh), par);
+        asm volatile("cp.async.wait_group %0;" ::"n"(TC_JOBS - 1) : "memory");   // this job's codes (each lane its own)
+        if (!warp_saw(free) && !warp_wait(TC_BAR(a_empty, kh), par, &sh->poison, g_linear_status, 1, s)) break;
+        tc_fence_after();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t to = R.tm + ((uint32_t)(32 * q + 16 * (i & 1)) << 16) + 128 * kh + 64 * (i >> 1);
+            const uint4 v0 = lds128(mine + job * 4096 + i * 1024), v1 = lds128(mine + job * 4096 + i * 1024 + 512);
+            const uint32_t cw[2][4] = {{v0.x, v0.y, v0.z, v0.w}, {v1.x, v1.y, v1.z, v1.w}};
+            uint32_t r[32];   // words in pairs of columns: register 4 j + 2 e (+ 1) is row gid + 8 e, pairs 2 j, 2 j + 1
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t w = cw[e][j >> 1];
+                    r[4 * j + 2 * e] = j & 1 ? code_pair<2>(w, bits) : code_pair<0>(w, bits);
+                    r[4 * j + 2 * e + 1] = j & 1 ? code_pair<3>(w, bits) : code_pair<1>(w, bits);
+                }
+            tc_st_x8(to, r);
+        }
+        bring(job);   // into the place of the codes that have just been stored
+        job = job + 1 == TC_JOBS ? 0 : job + 1;
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(TC_BAR(a_full, kh));
+    }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+// The MMAs of a group, both row tiles: G / 16 steps of 16 indices, A columns 8 k, B octets 2 k.  The first starts from zero.
+#define LIN_MMA(d, a, k, acc)                                            \
+    "add.s64 bd, %4, " #k "*%6;\n\tadd.s32 aa, " a ", " #k "*8;\n\t"     \
+    "@q tcgen05.mma.cta_group::1.kind::f16 [" d "], [aa], bd, %5, " acc ";\n\t"
+#define LIN_MMA4(d, a, k0, k1, k2, k3, first) \
+    LIN_MMA(d, a, k0, first) LIN_MMA(d, a, k1, "p1") LIN_MMA(d, a, k2, "p1") LIN_MMA(d, a, k3, "p1")
+#define LIN_HEAD                                                                                                       \
+    "{\n\t.reg .pred q, p0, p1;\n\t.reg .b64 bd;\n\t.reg .b32 aa;\n\telect.sync _|q, 0xffffffff;\n\t"                  \
+    "setp.ne.b32 p0, 0, 0;\n\tsetp.eq.b32 p1, 0, 0;\n\t"
+template <int G, int STEP>
+__device__ __forceinline__ void linear_mmas(uint32_t d0, uint32_t d1, uint32_t a0, uint32_t a1, uint64_t bd, uint32_t idesc) {
+    if constexpr (G == 128)
+        asm volatile(LIN_HEAD LIN_MMA4("%0", "%2", 0, 1, 2, 3, "p0") LIN_MMA4("%0", "%2", 4, 5, 6, 7, "p1")
+                         LIN_MMA4("%1", "%3", 0, 1, 2, 3, "p0") LIN_MMA4("%1", "%3", 4, 5, 6, 7, "p1") "}" ::"r"(d0),
+                     "r"(d1), "r"(a0), "r"(a1), "l"(bd), "r"(idesc), "n"(STEP)
+                     : "memory");
+    else
+        asm volatile(LIN_HEAD LIN_MMA4("%0", "%2", 0, 1, 2, 3, "p0") LIN_MMA4("%1", "%3", 0, 1, 2, 3, "p0") "}" ::"r"(d0), "r"(d1),
+                     "r"(a0), "r"(a1), "l"(bd), "r"(idesc), "n"(STEP)
+                     : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+        : "memory");
+}
+template <int TOK, int G>
+__device__ __noinline__ void tc_mma_role(const LinearArgs& a, TcRole R) {
+    using S = TcShape<TOK, G>;
+    constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TOK / 8) << 17) | ((128u / 16) << 24);   // fp32 += bf16 x bf16
+    const int K = a.K;
+    TcShared* const sh = R.S;
+    uint32_t buf = 0, par = 0;   // next accumulator buffer, parity of its round
+    uint32_t ready = 0;          // the next stage's barriers, asked for before this stage's MMAs are issued
+    TcPos pos(R);
+    for (int s = 0; s < R.n; ++s, pos.step(R)) {
+        const int slot = s % TC_SLOTS;
+        if (!warp_saw(ready) && (!warp_wait(TC_BAR(x_full, slot), (s / TC_SLOTS) & 1, &sh->poison, g_linear_status, 2, s) ||
+                                 !warp_wait(TC_BAR(a_full, s & 1), (s >> 1) & 1, &sh->poison, g_linear_status, 3, s)))
+            return;
+        ready = bar_test(TC_BAR(x_full, (s + 1) % TC_SLOTS), ((s + 1) / TC_SLOTS) & 1) & bar_test(TC_BAR(a_full, (s + 1) & 1), ((s + 1) >> 1) & 1);
+        const int ng = stage_groups<G>(pos.u, K);
+        for (int g = 0; g < ng; ++g) {
+            if (!warp_wait(TC_BAR(acc_empty, buf), par ^ 1, &sh->poison, g_linear_status, 4, s)) return;
+            tc_fence_after();
+            // (the shuffles tell the compiler that the operands are warp-uniform)
+            const uint32_t d = __shfl_sync(0xffffffffu, R.tm + 256 + buf * (2 * TOK), 0);
+            const uint32_t at = __shfl_sync(0xffffffffu, R.tm + 128 * (s & 1) + (G / 2) * g, 0);
+            const uint32_t xu = __shfl_sync(0xffffffffu, R.ring + slot * S::XB + g * (G / 8) * S::LBO, 0);
+            linear_mmas<G, 2 * S::LBO / 16>(d, d + TOK, at, at + 64, tc_desc(xu, S::LBO, 128), IDESC);
+            tc_commit(TC_BAR(acc_full, buf));
+            if (++buf == S::BUFS) buf = 0, par ^= 1;
+        }
+        tc_commit(TC_BAR(a_empty, s & 1));
+        tc_commit(TC_BAR(x_empty, slot));
+    }
+}
+
+// Sixteen consecutive values that all lanes read, as pairs, asked for together.
+__device__ __forceinline__ void lds_pairs16(uint32_t a, F2 (&v)[8]) {
+    asm volatile(
+        "ld.shared.v2.b64 {%0,%1}, [%8];\n\tld.shared.v2.b64 {%2,%3}, [%8+16];\n\t"
+        "ld.shared.v2.b64 {%4,%5}, [%8+32];\n\tld.shared.v2.b64 {%6,%7}, [%8+48];"
+        : "=l"(v[0].v), "=l"(v[1].v), "=l"(v[2].v), "=l"(v[3].v), "=l"(v[4].v), "=l"(v[5].v), "=l"(v[6].v), "=l"(v[7].v)
+        : "r"(a)
+        : "memory");
+}
+template <int TOK, int G, typename TO>
+__device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw, int lane) {
+    using S = TcShape<TOK, G>;
+    constexpr int NC = S::NC;
+    const int q = fw & 3, mt = (fw >> 2) & 1, col0 = (fw >> 3) * NC;
+    const int K = a.K, N = a.N, groups = K / G, row_in = 128 * mt + 32 * q + lane;
+    const uint32_t* const params = a.params;
+    TcShared* const sh = R.S;
+    F2 total[NC / 2];
+#pragma unroll
+    for (int c = 0; c < NC / 2; ++c) total[c] = f2(0.f);
+    TcPos pos(R), ahead(R);
+    const uint32_t* from;   // parameters of the lane's row in the block ahead
+    auto block_ahead = [&]() { from = params + (long long)min(ahead.n0 + row_in, N - 1) * groups; };
+    block_ahead();
+    uint32_t pr[S::GROUPS];
+    auto load_params = [&]() {   // of the stage `ahead`
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g) pr[g] = g < stage_groups<G>(ahead.u, K) ? __ldg(from + ahead.u * S::GROUPS + g) : 0u;
+        if (ahead.step(R)) block_ahead();
+    };
+    if (R.n > 0) load_params();
+    bool ok = true;
+    uint32_t buf = 0, par = 0, ready = 0;
+    const int u_first = pos.u;   // a first block that does not begin with its first stage is a piece
+    int piece = 0;
+    for (int s = 0; s < R.n; ++s) {
+        const int slot = s % TC_SLOTS, ng = stage_groups<G>(pos.u, K);
+        float s1[S::GROUPS], m1[S::GROUPS];
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g) {
+            const __half2 pv = *reinterpret_cast<const __half2*>(&pr[g]);
+            s1[g] = __low2float(pv);
+            m1[g] = fmaf(-16.f, s1[g], __high2float(pv));
+        }
+        if (s + 1 < R.n) load_params();
+        if (ok) ok = warp_saw(ready) || warp_wait(TC_BAR(x_full, slot), (s / TC_SLOTS) & 1, &sh->poison, g_linear_status, 5, s);
+        uint32_t full = bar_test(TC_BAR(acc_full, buf), par);
+        ready = bar_test(TC_BAR(x_full, (s + 1) % TC_SLOTS), ((s + 1) / TC_SLOTS) & 1);
+        // zero-points times the sums, as soon as the copies have landed (a group that is not there: m = 0, sums of zeros)
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g) {
+            const F2 m2 = f2(m1[g]);
+#pragma unroll
+            for (int c0 = 0; c0 < NC; c0 += 16) {
+                F2 x[8];
+                lds_pairs16(R.ring + slot * S::XB + 16 * S::LBO + (g * TOK + col0 + c0) * 4, x);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) total[c0 / 2 + c] = fma2(m2, x[c], total[c0 / 2 + c]);
+            }
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(TC_BAR(x_empty, slot));
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g) {
+            if (g >= ng) break;
+            if (ok) ok = warp_saw(full) || warp_wait(TC_BAR(acc_full, buf), par, &sh->poison, g_linear_status, 6, s);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t acc = R.tm + ((uint32_t)(32 * q) << 16) + 256 + buf * (2 * TOK) + mt * TOK + col0;
+            const F2 sg = f2(s1[g]);
+            uint32_t r[2][16];
+            tc_ld_rows16(acc, r[0]);
+#pragma unroll
+            for (int c0 = 0; c0 < NC; c0 += 16) {
+                uint32_t(&rr)[16] = r[(c0 / 16) & 1];
+                // (with the registers: what is read of them stays behind the wait)
+                asm volatile("tcgen05.wait::ld.sync.aligned;"
+                             : "+r"(rr[0]), "+r"(rr[1]), "+r"(rr[2]), "+r"(rr[3]), "+r"(rr[4]), "+r"(rr[5]), "+r"(rr[6]), "+r"(rr[7]), "+r"(rr[8]),
+                               "+r"(rr[9]), "+r"(rr[10]), "+r"(rr[11]), "+r"(rr[12]), "+r"(rr[13]), "+r"(rr[14]), "+r"(rr[15])
+                             :
+                             : "memory");
+                if (c0 + 16 < NC) {
+                    tc_ld_rows16(acc + c0 + 16, r[(c0 / 16 + 1) & 1]);
+                } else {   // the buffer is read: hand it back
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(TC_BAR(acc_empty, buf));
+                    if (++buf == S::BUFS) buf = 0, par ^= 1;
+                    if (g + 1 < ng) full = bar_test(TC_BAR(acc_full, buf), par);
+                }
+#pragma unroll
+                for (int c = 0; c < 16; c += 2)
+                    total[(c0 + c) / 2] = fma2(sg, f2(__uint_as_float(rr[c]), __uint_as_float(rr[c + 1])), total[(c0 + c) / 2]);
+            }
+        }
+        if (pos.u + 1 == R.stages || s + 1 == R.n) {
+            // the block's end, or the run's: a row a lane, so a column's stores of a warp are 32 consecutive values
+            const bool whole = pos.u + 1 == R.stages && (piece || u_first == 0);
+            const int t0 = pos.tile * TOK + col0, row = pos.n0 + row_in;
+            float* part = a.part + ((long long)(2 * blockIdx.x + (piece ? 1 : 0)) * TOK + col0) * TC_ROWS + row_in;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const float v = !ok ? __int_as_float(0x7fffffff) : c & 1 ? hi(total[c / 2]) : lo(total[c / 2]);
+                if (!whole) part[c * TC_ROWS] = v;
+                else store_y<TO>(a, t0 + c, row, v);
+            }
+#pragma unroll
+            for (int c = 0; c < NC / 2; ++c) total[c] = f2(0.f);
+            piece = 1;
+        }
+        pos.step(R);
+    }
+    if (!ok) sh->poison = 1;
+}
+
+template <int TOK, int G, typename TO>
+__global__ void __launch_bounds__(32 * TcShape<TOK, G>::WARPS, 1) linear_tc_kernel(const __grid_constant__ LinearArgs a) {
+    using S = TcShape<TOK, G>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ TcShared sh;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < TC_SLOTS; ++i) {
+            mbar_init(&sh.x_full[i], 1);
+            mbar_init(&sh.x_empty[i], S::FOLDS + 1);   // the fold warps have read the sums, and the MMAs are complete
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.a_full[i], 4);
+            mbar_init(&sh.a_empty[i], 1);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&sh.acc_full[i], 1);
+            mbar_init(&sh.acc_empty[i], S::FOLDS);
+        }
+        sh.poison = 0;
+        fence_barrier_init();
+    }
+    if (warp == S::W_MMA) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "n"(TC_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // Everything above runs beside the kernel that lays the activations out (all before that one has completed).
+    pdl_wait();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tm = tmem_at;
-    const uint32_t lanes = (uint32_t)(32 * q) << 16;
-    F2 acc[NC / 2];
-#pragma unroll
-    for (int c = 0; c < NC / 2; ++c) acc[c] = f2(0.f);
-    bool dead = false;
+    TcRole R;
+    R.S = &sh;
+    R.sb = smem_u32(&sh);
+    R.codes = smem_u32(smem);
+    R.ring = R.codes + S::CODES;
+    R.tm = __shfl_sync(0xffffffffu, sh.tmem, 0);
+    R.stages = (a.K + LIN_UNIT - 1) / LIN_UNIT;
+    R.blocks = (a.N + TC_ROWS - 1) / TC_ROWS;
+    R.first = tc_first(blockIdx.x, gridDim.x, a.units);
+    R.n = tc_first(blockIdx.x + 1, gridDim.x, a.units) - R.first;
+    if (warp < 8) {
+        tc_expand_role<G>(a, R, warp, lane);
+    } else if (warp < S::W_FETCH) {
+        tc_fold_role<TOK, G, TO>(a, R, warp - 8, lane);
+    } else if (warp == S::W_FETCH) {
+        if (lane == 0) {
+            TcPos pos(R);
+            bool ok = true;
+            for (int s = 0; s < R.n && ok; ++s, pos.step(R)) {
+                const int slot = s % TC_SLOTS;
+                if (s >= TC_SLOTS)
+                    ok = mbar_wait_bounded(&sh.x_empty[slot], ((s / TC_SLOTS) & 1) ^ 1, &sh.poison, g_linear_status, WAIT_LIMIT_NS, 7, s);
+                if (!ok) break;
+                mbar_arrive_expect_tx(&sh.x_full[slot], S::XB);
+                bulk_g2s(smem + S::CODES + slot * S::XB, a.xt + ((long long)pos.tile * R.stages + pos.u) * S::XB, S::XB, &sh.x_full[slot]);
+            }
+            if (!ok) {   // let copies in flight land before the CTA's shared memory goes away
+                const unsigned long long t = globaltimer_ns();
+                while (globaltimer_ns() - t < 2000000ull) {
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        tc_mma_role<TOK, G>(a, R);
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == S::W_MMA) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(R.tm), "n"(TC_COLS) : "memory");
+    }
+}
 
-    auto fill = [&](int i, int b) {   // stage i into buffers b; the MMAs that read them last are complete
-        if (brings) {
-            float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < S::TPW; ++j) {
-                mma_bf16(s4, BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, xv[j].x, xv[j].y);
-                mma_bf16(s4, BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, xv[j].z, xv[j].w);
-                // chunk (t, wd): the indices 8 (W t + wd) .. of the group, a lane t's word wd of the codes.  The 16x256b store gives
-                // the lane's pairs 2 j, 2 j + 1 the columns 8 j + 2 t, + 1, half t & 1 of the octet 2 j + (t >> 1).
-                uint32_t p[4];
-                b_operands(p, xv[j]);
-                const int c = 4 * (i0 + j) + tid4, t = c / W, wd = c % W;
-                const uint32_t at = smem_u32(smem) + b * S::XBUF + (4 * wd + (t >> 1)) * S::LBO + tok * 16 + 8 * (t & 1);
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(p[0]), "r"(p[1]) : "memory");
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at + 2 * S::LBO), "r"(p[2]), "r"(p[3]) : "memory");
-            }
-            if (lane < 4) *reinterpret_cast<float2*>(&sums[i % 3][warp / S::OCTETS][8 * oct + 2 * lane]) = make_float2(s4[0], s4[1]);
-        }
-        load_x(i + 1);
-        uint32_t r[8 * W];
-#pragma unroll
-        for (int j = 0; j < 2 * W; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t w = cw[b][e][j >> 1];
-                r[4 * j + 2 * e] = j & 1 ? code_pair<2>(w, a.bits) : code_pair<0>(w, a.bits);
-                r[4 * j + 2 * e + 1] = j & 1 ? code_pair<3>(w, a.bits) : code_pair<1>(w, a.bits);
-            }
-        if constexpr (W == 4) tc_st_x8(tm + ((uint32_t)(32 * q + 16 * h) << 16) + b * S::A_COLS, r);
-        else tc_st_x4(tm + ((uint32_t)(32 * q + 16 * h) << 16) + b * S::A_COLS, r);
-        load_codes(cw[b], i + 2);
-        tc_wait_st();
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the activations' stores, before the MMAs read them
-        tc_fence_before();
-    };
-    auto issue = [&](int b) {
-        tc_fence_after();
-        const uint64_t bd = tc_desc(smem_u32(smem) + b * S::XBUF, S::LBO, 128);
-        constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TOK / 8) << 17) | ((128u / 16) << 24);
-        linear_mmas<G, 2 * S::LBO / 16>(__shfl_sync(0xffffffffu, tm + 2 * S::A_COLS + b * TOK, 0), __shfl_sync(0xffffffffu, tm + b * S::A_COLS, 0),
-                                        bd, idesc, smem_u32(&bars[b]));
-    };
-    auto fold = [&](int i, int b) {
-        if (!dead) dead = !warp_wait(smem_u32(&bars[b]), (i >> 1) & 1, &poison, g_linear_status, 1, i);
-        tc_fence_after();
-        const uint32_t from = tm + lanes + 2 * S::A_COLS + b * TOK + h * NC;
-        uint32_t r[NC];
-#pragma unroll
-        for (int c = 0; c < NC; c += 8) tc_ld_rows8(from + c, r + c);
-        const uint32_t pw = params[(i >> 3) & 1][i & 7][32 * q + lane];
-        const __half2 pv = *reinterpret_cast<const __half2*>(&pw);
-        const float s1 = __low2float(pv);
-        const F2 s2 = f2(s1), m2 = f2(fmaf(-16.f, s1, __high2float(pv)));
-#pragma unroll
-        for (int c = 0; c < NC; c += 4)
-#pragma unroll
-            for (int sp = 0; sp < S::SPLITS; ++sp) {
-                const float4 v = *reinterpret_cast<const float4*>(&sums[i % 3][sp][h * NC + c]);
-                acc[c / 2] = fma2(m2, f2(v.x, v.y), acc[c / 2]);
-                acc[c / 2 + 1] = fma2(m2, f2(v.z, v.w), acc[c / 2 + 1]);
-            }
-        tc_wait_ld();
-#pragma unroll
-        for (int c = 0; c < NC; c += 8)   // (what is read of them stays behind the wait)
-            asm volatile("" : "+r"(r[c]), "+r"(r[c + 1]), "+r"(r[c + 2]), "+r"(r[c + 3]), "+r"(r[c + 4]), "+r"(r[c + 5]), "+r"(r[c + 6]), "+r"(r[c + 7]));
-#pragma unroll
-        for (int c = 0; c < NC; c += 2) acc[c / 2] = fma2(s2, f2(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), acc[c / 2]);
-        tc_fence_before();
-    };
-    fill(0, 0);
-    __syncthreads();
-    if (warp == 0) issue(0);
-    for (int i = 0; i < n; i += 2) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            if (i + b >= n) break;
-            // the next eight groups' parameters: asked for at the second stage of eight (every warp has folded the eight before, whose
-            // place they take), there at the last
-            if (((i + b) & 7) == 1 && (((i + b) >> 3) + 1) * 8 < n) bring_params(((i + b) >> 3) + 1);
-            if (i + b + 1 < n) {
-                fill(i + b + 1, b ^ 1);
-                if (((i + b) & 7) == 7) asm volatile("cp.async.wait_group 0;" ::: "memory");
-                __syncthreads();   // stage i + b + 1 is filled, stage i + b - 1 folded by every warp
-                if (warp == 0) issue(b ^ 1);
-            }
-            fold(i + b, b);
-        }
+// The blocks whose stages several CTAs took: their pieces added up in the order of the CTAs.  grid (block over all token tiles,
+// four tokens); four rows a thread.
+template <int TOK, typename TO>
+__global__ void __launch_bounds__(256) linear_pieces_kernel(const __grid_constant__ LinearArgs a, int ctas, int stages, int blocks) {
+    pdl_wait();
+    const int block = blockIdx.x, first = block * stages;
+    // the CTAs whose runs hold the block's first and last stage; a block other than a CTA's first is its last piece
+    int c0 = (int)((long long)first * ctas / a.units);
+    while (tc_first(c0 + 1, ctas, a.units) <= first) ++c0;
+    if (tc_first(c0 + 1, ctas, a.units) >= first + stages) return;   // one CTA's: written by it
+    int c1 = c0 + 1;
+    while (tc_first(c1 + 1, ctas, a.units) < first + stages) ++c1;
+    const int slot0 = tc_first(c0, ctas, a.units) >= first ? 0 : 1;
+    const int t = 4 * blockIdx.y + (threadIdx.x >> 6), row = 4 * (threadIdx.x & 63);
+    const int n = block % blocks * TC_ROWS + row, t0 = block / blocks * TOK;
+    if (t0 + t >= a.T) return;
+    const float* part = a.part + (long long)t * TC_ROWS + row;
+    float4 v = *reinterpret_cast<const float4*>(part + (long long)(2 * c0 + slot0) * (TOK * TC_ROWS));
+#pragma unroll 4
+    for (int c = c0 + 1; c <= c1; ++c) {
+        const float4 w = *reinterpret_cast<const float4*>(part + (long long)(2 * c) * (TOK * TC_ROWS));
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
     }
-    __syncthreads();
-    if (warp == 0) {
-        tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "n"(S::COLS) : "memory");
-    }
-    // results to shared memory, [token][row], then out in whole rows of a token
-    const bool bad = *(volatile int*)&poison;
-    float* part = reinterpret_cast<float*>(smem);
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-        part[(h * NC + c) * TC_ROWS + 32 * q + lane] = bad ? __int_as_float(0x7fffffff) : (c & 1 ? hi(acc[c / 2]) : lo(acc[c / 2]));
-    if (a.n_split == 1) {
-        __syncthreads();
-        for (int o = tid; o < TOK * TC_ROWS; o += THREADS) store_y<TO>(a, t0 + o / TC_ROWS, n0 + o % TC_ROWS, part[o]);
-        return;
-    }
-    cluster_sync_all();
-    for (int o = split * THREADS + tid; o < TOK * TC_ROWS; o += a.n_split * THREADS)
-        store_y<TO>(a, t0 + o / TC_ROWS, n0 + o % TC_ROWS, cluster_sum(part, o, a.n_split));
-    cluster_sync_all();
+    store_y<TO>(a, t0 + t, n, v.x);
+    store_y<TO>(a, t0 + t, n + 1, v.y);
+    store_y<TO>(a, t0 + t, n + 2, v.z);
+    store_y<TO>(a, t0 + t, n + 3, v.w);
 }
 
 // Shares of the input indices, a CTA of a cluster each: as many as leave the fewest units to the SM with most work.
-#ifndef LIN_OVER
-#define LIN_OVER 12
-#endif
-#ifndef LIN_FEW
-#define LIN_FEW 16
-#endif
 static void split_units(LinearArgs& a, int units, long long blocks, int n_sms, int per_sm, int least, int start) {
     int best = 1;
     double best_cost = 1e30;
@@ -578,22 +806,56 @@ static cudaError_t linear_few(LinearArgs a, int y_f32, int n_sms, cudaStream_t s
     return y_f32 ? launch_pdl_cluster(linear_few_kernel<NT, R, U, G, float>, grid, dim3(32 * LIN_WARPS), 0, a.n_split, st, a)
                  : launch_pdl_cluster(linear_few_kernel<NT, R, U, G, __nv_bfloat16>, grid, dim3(32 * LIN_WARPS), 0, a.n_split, st, a);
 }
+// Tokens of a tile of the tcgen05 kernel; 0: the call is the few-token kernel's.
+// The few-token kernel reads the matrix once a tile of 16 tokens and its warps multiply each tile anew, but it is one launch with
+// nothing to set up; the tcgen05 kernel has two launches beside it and the start of its pipeline, about 10 us, and then takes
+// twice the codes in the same time.  So the rule is on the weights times the tiles of 16 (us, few-token against tcgen05):
+//   2^20 2.9 / 10.1,  2^24 6.4 / 12.1 (64 tokens, 2048 x 2048),  2^25 10.6 / 15.8 (64, 2048 x 4096) and 10.9 / 14.8 (32, 4096 x 4096),
+//   56 * 2^20 20.0 / 19.3 (16, 14336 x 4096),  2^26 18.8 / 18.9 (16, 8192 x 8192) and 21.1 / 19.0 (64, 4096 x 4096),
+//   2^27 35.9 / 20.3 (128, 4096 x 4096),  196 * 2^20 57.4 / 39.3 (16, 14336 x 14336).
+// With 8 tokens the few-token kernel has one MMA a step and keeps up with the codes: 41.3 us at 14336 x 14336, the other 39.0 us.
+static int tc_tile(int T, int rows, int cols) {
+    if (T <= 8 || (T + 15) / 16 * (long long)rows * cols <= 3ll << 24) return 0;
+    return T <= 16 ? 16 : T <= 32 ? 32 : 64;
+}
+static size_t tc_x_bytes(int T, int cols, int G, int tok) {
+    const size_t n = (size_t)((T + tok - 1) / tok) * ((cols + LIN_UNIT - 1) / LIN_UNIT) * (16 * 16 * tok + LIN_UNIT / G * tok * 4);
+    return (n + 255) / 256 * 256;
+}
+static size_t tc_workspace(int T, int rows, int cols, int G) {
+    const int tok = tc_tile(T, rows, cols);
+    return tok ? tc_x_bytes(T, cols, G, tok) + (size_t)TC_MAX_CTAS * 2 * tok * TC_ROWS * 4 : 0;
+}
 template <int TOK, int G>
 static cudaError_t linear_tc(LinearArgs a, int y_f32, int n_sms, cudaStream_t st) {
     constexpr int SMEM = TcShape<TOK, G>::SMEM;
-    const unsigned blocks = (unsigned)((a.N + TC_ROWS - 1) / TC_ROWS), tiles = (unsigned)((a.T + TOK - 1) / TOK);
-    split_units(a, a.K / G, (long long)blocks * tiles, n_sms, 2, 4, LIN_OVER);
-    const dim3 grid(blocks * a.n_split, tiles);
-    auto go = [&](auto kernel) { return launch_pdl_cluster(kernel, grid, dim3(32 * LIN_WARPS), SMEM, a.n_split, st, a); };
-    return y_f32 ? go(linear_tc_kernel<TOK, G, float>) : go(linear_tc_kernel<TOK, G, __nv_bfloat16>);
+    const int stages = (a.K + LIN_UNIT - 1) / LIN_UNIT, blocks = (a.N + TC_ROWS - 1) / TC_ROWS, tiles = (a.T + TOK - 1) / TOK;
+    const long long warps = (long long)tiles * (TOK / 8) * stages, units = (long long)tiles * blocks * stages;
+    a.part = reinterpret_cast<float*>(const_cast<uint8_t*>(a.xt) + tc_x_bytes(a.T, a.K, G, TOK));
+    a.units = (int)units;
+    cudaError_t e = launch_pdl(linear_x_kernel<TOK, G>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a.x, a.T, a.K, stages, tiles,
+                               const_cast<uint8_t*>(a.xt));
+    if (e != cudaSuccess) return e;
+    // a run of two stages at least
+    const int ctas = (int)std::max(1ll, std::min({(long long)n_sms, (long long)TC_MAX_CTAS, units / 2}));
+    auto go = [&](auto kernel, auto pieces) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        if (e == cudaSuccess) e = launch_pdl(kernel, dim3((unsigned)ctas), dim3(32 * TcShape<TOK, G>::WARPS), SMEM, st, a);
+        if (e == cudaSuccess) e = launch_pdl(pieces, dim3((unsigned)(blocks * tiles), TOK / 4), dim3(256), 0, st, a, ctas, stages, blocks);
+        return e;
+    };
+    return y_f32 ? go(linear_tc_kernel<TOK, G, float>, linear_pieces_kernel<TOK, float>)
+                 : go(linear_tc_kernel<TOK, G, __nv_bfloat16>, linear_pieces_kernel<TOK, __nv_bfloat16>);
 }
 template <int G>
 static cudaError_t linear_by_tokens(const LinearArgs& a, int y_f32, int n_sms, cudaStream_t st) {
-    if (a.T <= LIN_FEW && a.T <= 8) return a.N >= 64 * n_sms ? linear_few<1, 2, 2, G>(a, y_f32, n_sms, st) : linear_few<1, 1, 4, G>(a, y_f32, n_sms, st);
-    if (a.T <= LIN_FEW) return linear_few<2, 2, 2, G>(a, y_f32, n_sms, st);
-    if (a.T <= 16) return linear_tc<16, G>(a, y_f32, n_sms, st);
-    if (a.T <= 32) return linear_tc<32, G>(a, y_f32, n_sms, st);
-    return linear_tc<64, G>(a, y_f32, n_sms, st);
+    switch (tc_tile(a.T, a.N, a.K)) {
+        case 16: return linear_tc<16, G>(a, y_f32, n_sms, st);
+        case 32: return linear_tc<32, G>(a, y_f32, n_sms, st);
+        case 64: return linear_tc<64, G>(a, y_f32, n_sms, st);
+    }
+    if (a.T <= 8) return a.N >= 64 * n_sms ? linear_few<1, 2, 2, G>(a, y_f32, n_sms, st) : linear_few<1, 1, 4, G>(a, y_f32, n_sms, st);
+    return linear_few<2, 2, 2, G>(a, y_f32, n_sms, st);
 }
 
 }  // namespace dyn
@@ -604,7 +866,7 @@ namespace {
 
 dynamo_status check_linear(int32_t rows, int32_t cols, int32_t group_size) {
     if (group_size != 64 && group_size != 128) return DYNAMO_ERR_SHAPE;
-    if (rows < 1 || cols < group_size || cols % group_size || cols > 1 << 24) return DYNAMO_ERR_SHAPE;   // (offsets of 32 bits)
+    if (rows < 1 || cols < group_size || cols % group_size || cols > 1 << 24 || rows > 1 << 24) return DYNAMO_ERR_SHAPE;   // (offsets of 32 bits)
     return DYNAMO_OK;
 }
 
@@ -625,6 +887,14 @@ dynamo_status dynamo_linear_quantize(const void* w, int32_t rows, int32_t cols, 
                : DYNAMO_ERR_CUDA;
 }
 
+dynamo_status dynamo_linear_workspace_bytes(int32_t T, int32_t rows, int32_t cols, int32_t group_size, size_t* bytes) {
+    if (const dynamo_status s = check_linear(rows, cols, group_size); s != DYNAMO_OK) return s;
+    if (!bytes) return DYNAMO_ERR_NULL;
+    if (T < 0 || T > DYNAMO_LINEAR_MAX_TOKENS) return DYNAMO_ERR_TOKENS;
+    *bytes = tc_workspace(T, rows, cols, group_size);
+    return DYNAMO_OK;
+}
+
 dynamo_status dynamo_linear_poll_status(void* stream) {
     if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return DYNAMO_ERR_CUDA;
     int32_t word = 0;
@@ -636,16 +906,23 @@ dynamo_status dynamo_linear_poll_status(void* stream) {
 }
 
 dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size, const void* codes,
-                                    const void* params, void* y, int32_t y_dtype, void* stream) {
+                                    const void* params, void* y, int32_t y_dtype, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
     if (const dynamo_status s = check_linear(rows, cols, group_size); s != DYNAMO_OK) return s;
     if (y_dtype != DYNAMO_BF16 && y_dtype != DYNAMO_F32) return DYNAMO_ERR_SHAPE;
     if (T < 0 || T > DYNAMO_LINEAR_MAX_TOKENS) return DYNAMO_ERR_TOKENS;
     if (T == 0) return DYNAMO_OK;
     if (!x || !codes || !params || !y) return DYNAMO_ERR_NULL;
     if (!aligned16(x, codes, params, y)) return DYNAMO_ERR_ALIGN;
+    // (the tcgen05 kernel counts its stages, a tile of tokens by 256 rows by 128 columns each, in 32 bits)
+    if ((long long)(T / 16 + 1) * (rows / 256 + 1) * (cols / 128 + 1) > 0x7fffffffll) return DYNAMO_ERR_TOKENS;
+    const size_t need = tc_workspace(T, rows, cols, group_size);
+    if (need && !workspace) return DYNAMO_ERR_NULL;
+    if (workspace_bytes < need) return DYNAMO_ERR_ARENA_TOO_SMALL;
+    if (need && ((uintptr_t)workspace & 255)) return DYNAMO_ERR_ALIGN;
     int n_sms = 0;
     if (count_sms(&n_sms) != cudaSuccess) return DYNAMO_ERR_CUDA;
-    const LinearArgs a = {(const __nv_bfloat16*)x, (const uint8_t*)codes, (const uint32_t*)params, y, T, cols, rows, {0x00780078u, 0x41804180u}, 1, 0};
+    const LinearArgs a = {(const __nv_bfloat16*)x, (const uint8_t*)codes, (const uint32_t*)params, y, T, cols, rows, {0x00780078u, 0x41804180u}, (const uint8_t*)workspace, nullptr, 1, 0};
     const cudaError_t e = group_size == 64 ? linear_by_tokens<64>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream)
                                            : linear_by_tokens<128>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream);
     return e == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;

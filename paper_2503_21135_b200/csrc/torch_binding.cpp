@@ -440,7 +440,11 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
         like(y, "out", device, y_type);
         shaped(y, "out", {T, N});
     }
-    check_status(dynamo_linear_forward(ptr(x), T, N, K, G, ptr(codes), ptr(params), mut(y), type_code(y, "out"), on.stream),
+    size_t need = 0;
+    check_status(dynamo_linear_workspace_bytes(T, N, K, G, &need), "dynamo_linear_workspace_bytes");
+    Tensor ws;
+    if (need) ws = empty({(int64_t)need}, device, at::kByte);
+    check_status(dynamo_linear_forward(ptr(x), T, N, K, G, ptr(codes), ptr(params), mut(y), type_code(y, "out"), mut(ws), need, on.stream),
                  "dynamo_linear_forward");
     return wrap(y);
     END_HANDLE_TH_ERRORS

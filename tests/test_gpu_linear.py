@@ -61,6 +61,45 @@ def test_linear(T, N, K, G, y_dtype):
     assert torch.equal(out, y) and (guard[T] == 5.0).all()
 
 
+# Matrices and token counts behind the few-token kernel's: token tiles of 16, 32 and 64, partly filled; rows that end inside a block of
+# 256; a last step of 64 indices; blocks that one run of work holds, that two share, that all runs share.
+MANY = [(9, 14393, 4096), (16, 4099, 14336), (17, 6401, 4096), (31, 4096, 8128), (33, 4101, 4160), (64, 257, 49216), (64, 13000, 1024),
+        (65, 1000, 10304), (500, 1500, 1088), (4000, 250, 832), (20000, 130, 320), (20000, 700, 64), (65536, 33, 384)]
+
+
+@pytest.mark.parametrize("y_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("T,N,K", MANY)
+def test_linear_many(T, N, K, G, y_dtype):
+    """As above, but a result's groups are added up one behind the other (two roundings of 2^-24 each), then at most 32 pieces."""
+    K = max(K // G, 1) * G
+    w, x = make(T, N, K, G)
+    codes, params = ops.quantize_linear(w, G)
+    guard = torch.full((T + 1, N), 5.0, dtype=torch.float32 if y_dtype == "f32" else torch.bfloat16, device="cuda")
+    y = ops.linear(x, codes, params, y_dtype=binding.F32 if y_dtype == "f32" else binding.BF16, out=guard[:T])
+    assert binding.load().dynamo_linear_poll_status(None) == 0
+    q = torch.stack([codes & 15, codes >> 4], 2).view(N, K).double()
+    s, m = params.double().repeat_interleave(G, 1).unbind(2)
+    X = x.double()
+    ref, C = X @ (s * q + m).T, X.abs() @ (s.abs() * (16 + q) + (m - 16 * s).abs()).T
+    tol = (8 * 17 + K / G + 32) * 2.0 ** -23 * C + torch.finfo(y.dtype).eps / 2 * ref.abs()
+    assert bool(((y.double() - ref).abs() <= tol * 1.01).all()) and bool((guard[T] == 5.0).all())
+    assert torch.equal(ops.linear(x, codes, params, y_dtype=binding.F32 if y_dtype == "f32" else binding.BF16), y)
+
+
+def test_non_finite_rows_many():
+    """A token's infinity and NaN stay its own, in every tile."""
+    w, x = make(70, 12000, 1024, 128)
+    codes, params = ops.quantize_linear(w, 128)
+    y = ops.linear(x, codes, params)
+    want = y.clone()
+    x[3, 17], x[64, 300], x[69] = float("inf"), float("nan"), 0
+    y = ops.linear(x, codes, params)
+    rest = [i for i in range(69) if i not in (3, 64)]
+    assert torch.equal(y[rest], want[rest]) and (y[69] == 0).all()
+    assert not torch.isfinite(y[3]).any() and torch.isnan(y[64]).all()
+
+
 @pytest.mark.parametrize("G", [64, 128])
 @pytest.mark.parametrize("N,K", [(1, 128), (5, 384), (129, 1408), (64, 4096)])
 def test_quantizer_is_the_experts(N, K, G):
@@ -107,8 +146,9 @@ def test_far_apart_magnitudes_and_non_finite_rows():
     assert torch.isnan(y[1]).all() and not torch.isfinite(y[3]).any()
 
 
-def test_capture_and_streams():
-    w, x = make(8, 1000, 2048, 128)
+@pytest.mark.parametrize("T,N,K", [(8, 1000, 2048), (16, 14336, 4096), (40, 4352, 4096)])
+def test_capture_and_streams(T, N, K):
+    w, x = make(T, N, K, 128)
     codes, params = ops.quantize_linear(w, 128)
     want = ops.linear(x, codes, params)
     graphs, outs = [], []

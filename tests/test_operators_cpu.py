@@ -102,14 +102,21 @@ def test_linear_refusals(lib):
     def quant(w=P, N=8, K=128, G=64, c=P, p=P):
         return lib.dynamo_linear_quantize(w, N, K, G, c, p, None)
 
-    def fwd(x=P, T=1, N=8, K=128, G=64, c=P, p=P, y=P, ydt=0):
-        return lib.dynamo_linear_forward(x, T, N, K, G, c, p, y, ydt, None)
+    def fwd(x=P, T=1, N=8, K=128, G=64, c=P, p=P, y=P, ydt=0, ws=None, nb=0):
+        return lib.dynamo_linear_forward(x, T, N, K, G, c, p, y, ydt, ws, nb, None)
 
     for kw, st in ((dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(K=96), SHAPE), (dict(K=192, G=128), SHAPE), (dict(G=32), SHAPE),
                    (dict(c=None), NULL), (dict(p=None), NULL), (dict(c=P + 8), ALIGN), (dict(p=P + 4), ALIGN)):
         assert quant(**kw) == st and fwd(**kw) == st, kw
+    assert _bytes(lib.dynamo_linear_workspace_bytes, 1, 64, 256, 64) == (OK, 0)
+    assert _bytes(lib.dynamo_linear_workspace_bytes, 64, 8192, 8192, 64)[1] >= 64 * 8192 * 2
+    assert _bytes(lib.dynamo_linear_workspace_bytes, 64, 64, 200, 64)[0] == SHAPE
+    assert _bytes(lib.dynamo_linear_workspace_bytes, -1, 64, 256, 64)[0] == TOKENS
     assert quant(w=None) == NULL and quant(w=P + 2) == ALIGN
     assert fwd(x=None) == NULL and fwd(y=None) == NULL and fwd(x=P + 8) == ALIGN and fwd(ydt=7) == SHAPE
+    big = dict(T=40, N=8192, K=8192)
+    assert fwd(**big) == NULL and fwd(ws=P, nb=8, **big) == SMALL and fwd(ws=P + 16, nb=1 << 30, **big) == ALIGN
+    assert fwd(T=16, N=8, K=(1 << 24) + 64) == SHAPE and fwd(T=65536, N=1 << 24, K=1 << 24, ws=P, nb=1 << 40) == TOKENS
     assert fwd(T=-1) == TOKENS and fwd(T=binding.LINEAR_MAX_TOKENS + 1) == TOKENS and fwd(T=0, x=None, y=None) == OK
 
 
