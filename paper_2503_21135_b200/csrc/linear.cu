@@ -308,12 +308,15 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 //                  row's codes; a row a lane kept the L1 busy with 32 lines a load).  The codes come by cp.async, three jobs of a warp
 //                  on their way: 96 KB an SM (one job in registers left the loads' latency to bind)
 //   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + (m - 16 s) * sum(x), two columns an instruction;
-//                  sixteen warps at 64 tokens, half of the columns each: eight took 84 us where sixteen take less than the expansion
+//                  sixteen warps at 64 tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 90.7 / 53.2 us;
+//                  eight warps 107 / 50.6; sixteen of a quarter of the columns and both row tiles, half the reads of the sums: 109 / 54.6)
 //   next  fetch  : one thread; a bulk copy a stage of the activations, which linear_x_kernel has put into the operand's order,
 //                  with their sums per group behind them
 //   last  MMA    : 2 * 128 / 16 tcgen05.mma of 128 x TOK x 16 a stage, a run and one commit
 // Roles meet at barriers only, so that the chain of a stage (codes, expansion, MMAs, fold) overlaps its neighbours', blocks' ends
 // included; the same work by eight warps that all did every part, a barrier of the CTA a stage, took 88 us at 64 tokens, 14336 x 14336.
+// Bound by the fold at 64 tokens (2000 cycles a group's 256 x 64 results, two instructions a pair of them and the reads of accumulators and
+// sums), by the expansion and the hand-overs at 32 and fewer: 43.3 us, 39% of what the codes' bytes take.
 // A block that lies within one CTA's run goes from the fold warps' registers to y; the pieces of the others go to the workspace, and a
 // kernel behind this one adds them up in the order of the CTAs.
 // Tensor memory: two A buffers of 128 columns, then BUFS accumulator buffers of 2 * TOK, one a group.
