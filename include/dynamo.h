@@ -383,12 +383,13 @@ dynamo_status dynamo_route_permute_static(const float* router_logits, int32_t T,
                                           int32_t* expert_offsets, int32_t* perm, void* stream);
 
 /* ---- Operators around the layer --------------------------------------------------------------------------------------
- * What a decoder block needs next to dynamo_moe_forward.  They take no context: device buffers, sizes and a stream, which
- * has to belong to the current device.  Every call is asynchronous and stream-ordered, can be captured in a CUDA graph, keeps
- * nothing between calls and gives the same bits for the same inputs (no floating-point atomics).  Row-major contiguous
- * arrays, 16-byte aligned (ERR_ALIGN); a *_dtype is DYNAMO_BF16 or DYNAMO_F32 (ERR_SHAPE otherwise); widths are multiples of
- * 8 (ERR_SHAPE).  Outputs must not overlap inputs or one another unless stated.  Sums, norms and weights are worked out in
- * fp32, results rounded once.  T = 0 is a no-op unless stated.
+ * What a decoder block needs next to dynamo_moe_forward.  They take no context (but dynamo_moe_block_forward does):
+ * device buffers, sizes and a stream, which has to belong to the current device.  Every call is asynchronous and stream-
+ * ordered, can be captured in a CUDA graph, keeps nothing between calls and gives the same bits for the same inputs (no
+ * floating-point atomics).  Row-major contiguous arrays, 16-byte aligned (ERR_ALIGN); a *_dtype is DYNAMO_BF16 or
+ * DYNAMO_F32 (ERR_SHAPE otherwise); widths are multiples of 8 (ERR_SHAPE).  Outputs must not overlap inputs or one
+ * another unless stated.  Sums, norms and weights are worked out in fp32, results rounded once.  T = 0 is a no-op unless
+ * stated.
  *
  * Tokens sorted by expert and back (Section II-A: one-to-many dispatch; for experts other than the layer's own, and for
  * training what stands around them).
@@ -448,6 +449,16 @@ dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void
                                         const void* y, const float* stats, const void* w_post, const void* gate,
                                         const void* w_pre, int32_t T, void* d_r, void* d_y, float* d_w_post, float* d_gate,
                                         float* d_w_pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The layer as a decoder block has it: dynamo_moe_forward_router of n, then the join, both on the stream.
+ *   n bf16 [T, d] : the normalised stream, n_out of the join in front of this block (of dynamo_norm_join_forward without y for a
+ *                   stream's first); r [T, d] r_dtype the stream itself
+ *   y [T, d] y_dtype : the layer's output, written;  the other arguments as in the two calls.  r_out may be r, n_out may be n.
+ * What either call refuses is refused before anything is launched; desc->d has to be the layer's d_model (ERR_SHAPE). */
+dynamo_status dynamo_moe_block_forward(dynamo_ctx* ctx, const dynamo_join_desc* desc, const void* r, const void* n,
+                                       const void* w_router, const float* router_bias, const void* w_post, const void* gate,
+                                       const void* w_pre, int32_t T, void* y, void* r_out, void* n_out, float* stats,
+                                       float* logits_out, void* stream);
 
 /* Products with a 4-bit matrix that has group scales: the block's other projections, in the experts' quantizer.
  * dynamo_linear_quantize: w bf16 [rows, cols] -> codes uint8 [rows, cols / 2] (index 2i in the low, 2i + 1 in the high half of

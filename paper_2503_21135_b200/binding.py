@@ -41,6 +41,7 @@ EXPORTED = ["dynamo_create", "dynamo_destroy", "dynamo_arena_bytes", "dynamo_pac
             "dynamo_debug_expire_wait", "dynamo_debug_check_guards",
             "dynamo_dispatch_workspace_bytes", "dynamo_dispatch", "dynamo_combine", "dynamo_combine_backward",
             "dynamo_norm_join_forward", "dynamo_norm_join_workspace_bytes", "dynamo_norm_join_backward",
+            "dynamo_moe_block_forward",
             "dynamo_linear_quantize", "dynamo_linear_forward", "dynamo_linear_workspace_bytes",
             "dynamo_linear_poll_status",
             "dynamo_kernel_launches", "dynamo_status_str"]
@@ -118,6 +119,7 @@ def load():
         L.dynamo_norm_join_forward.argtypes = [jd, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
         L.dynamo_norm_join_workspace_bytes.argtypes = [jd, i32, ctypes.POINTER(sz)]
         L.dynamo_norm_join_backward.argtypes = [jd, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.dynamo_moe_block_forward.argtypes = [vp, jd, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
         L.dynamo_linear_quantize.argtypes = [vp, i32, i32, i32, vp, vp, vp]
         L.dynamo_linear_forward.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp, sz, vp]
         L.dynamo_linear_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
@@ -381,6 +383,43 @@ class DynamoLayer:
         _check(st, "dynamo_moe_forward_router")
         res = (y,) + ((lg,) if want_logits else ()) + ((outs,) if debug else ())
         return res if len(res) > 1 else y
+
+    def forward_block(self, r: torch.Tensor, n: torch.Tensor, w_router: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      w_post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                      w_pre: Optional[torch.Tensor] = None, post_norm: bool = True, pre_norm: bool = True, res_scale: float = 1.0,
+                      block_scale: float = 1.0, eps: float = 1e-6, y_dtype=F32, y: Optional[torch.Tensor] = None,
+                      in_place: bool = False):
+        """The layer and the join behind it: forward_router of n bf16 [T, d] (the normalised stream), its output normed, gated
+        and added to the stream r [T, d], and the norm in front of the next block.  Returns (r_out, n_out), n_out None without
+        pre_norm; in_place: r and n themselves.  gate: [d], or fp32 [T, 1].  y: a buffer [T, d] of y_dtype for the layer's output."""
+        T, d = r.shape
+        types = {torch.bfloat16: BF16, torch.float32: F32}
+        rows = [w for w in (w_post, w_pre) if w is not None]
+        per_token = gate is not None and gate.dim() == 2
+        if gate is not None and not per_token:
+            rows.append(gate)
+        given = [r, n, w_router] + [t for t in (bias, w_post, gate, w_pre, y) if t is not None]
+        assert all(t.is_cuda and t.is_contiguous() and t.device == self.workspace.device for t in given)
+        assert d == self.desc.d_model and r.dtype in types and n.shape == r.shape and n.dtype == torch.bfloat16
+        assert tuple(w_router.shape) == (self.desc.n_experts, d) and w_router.dtype == torch.bfloat16
+        assert bias is None or (bias.dtype == torch.float32 and bias.numel() == self.desc.n_experts)
+        assert all(w.shape == (d,) and w.dtype in types and w.dtype == rows[0].dtype for w in rows)
+        assert not per_token or (tuple(gate.shape) == (T, 1) and gate.dtype == torch.float32)
+        assert (post_norm or w_post is None) and (pre_norm or w_pre is None)
+        if y is None:
+            y = torch.empty((T, d), dtype=torch.float32 if y_dtype == F32 else torch.bfloat16, device=r.device)
+        assert y.shape == r.shape and types.get(y.dtype) == y_dtype
+        r_out = r if in_place else torch.empty_like(r)
+        n_out = None if not pre_norm else n if in_place else torch.empty_like(n)
+        kind = GATE_NONE if gate is None else GATE_TOKEN if per_token else GATE_CHANNEL
+        desc = JoinDesc(d, y_dtype, types[r.dtype], BF16, types[rows[0].dtype] if rows else BF16, kind, int(post_norm), int(pre_norm),
+                        res_scale, block_scale, eps)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        with torch.cuda.device(r.device):
+            st = load().dynamo_moe_block_forward(self.ctx, ctypes.byref(desc), ptr(r), ptr(n), ptr(w_router), ptr(bias), ptr(w_post),
+                                                 ptr(gate), ptr(w_pre), T, ptr(y), ptr(r_out), ptr(n_out), None, None, _stream())
+        _check(st, "dynamo_moe_block_forward")
+        return r_out, n_out
 
     def forward_host(self, x_host: torch.Tensor, logits_host: torch.Tensor, y_host: torch.Tensor, y_dtype=F32):
         T = x_host.shape[0]

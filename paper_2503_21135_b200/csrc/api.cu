@@ -31,6 +31,8 @@ cudaError_t launch_export(const LayerDev* L, int e, int mat, int which, long lon
                           uint16_t* zr, cudaStream_t st);
 cudaError_t launch_route(const float* logits, int T, int E, int k, int renorm, int32_t* idx, float* w,
                          cudaStream_t st);
+dynamo_status check_join_forward(const dynamo_join_desc* desc, const void* r, const void* y, const void* w_post, const void* gate,
+                                 const void* w_pre, int32_t T, const void* r_out, const void* n_out, const float* stats);
 cudaError_t launch_route_gemm(const void* x, const void* w_router, const float* bias, int T, int d, int E, int k,
                               int renorm, float* logits_out, int32_t* idx, float* w, cudaStream_t st);
 cudaError_t launch_upload(const void* xh, void* xd, long long x_bytes, const float* lh, float* ld, long long n_logits,
@@ -944,6 +946,20 @@ dynamo_status dynamo_moe_forward_router(dynamo_ctx* ctx, const void* x, const vo
                                         const dynamo_debug_out* dbg, void* stream) {
     if (ctx && ctx->packed && T > 0 && T <= ctx->D.max_tokens && !w_router) return DYNAMO_ERR_NULL;
     return forward_impl(ctx, x, nullptr, w_router, router_bias, logits_out, T, y, y_dtype, dbg, stream);
+}
+
+dynamo_status dynamo_moe_block_forward(dynamo_ctx* ctx, const dynamo_join_desc* desc, const void* r, const void* n, const void* w_router,
+                                       const float* router_bias, const void* w_post, const void* gate, const void* w_pre, int32_t T,
+                                       void* y, void* r_out, void* n_out, float* stats, float* logits_out, void* stream) {
+    if (!ctx || !desc) return DYNAMO_ERR_NULL;
+    if (desc->d != ctx->D.d_model) return DYNAMO_ERR_SHAPE;
+    if (T > 0 && !y) return DYNAMO_ERR_NULL;   // (to the join a missing y is a block that is not there)
+    if (const dynamo_status s = check_join_forward(desc, r, y, w_post, gate, w_pre, T, r_out, n_out, stats); s != DYNAMO_OK) return s;
+    if (const dynamo_status s = dynamo_moe_forward_router(ctx, n, w_router, router_bias, T, y, desc->y_dtype, logits_out, nullptr, stream);
+        s != DYNAMO_OK || T == 0)
+        return s;
+    ctx->launches += 1;
+    return dynamo_norm_join_forward(desc, r, y, w_post, gate, w_pre, T, r_out, n_out, stats, stream);
 }
 
 // Start and size of the allocation or registration that a device address belongs to; false where the driver has none.

@@ -505,11 +505,10 @@ JoinArgs join_args(const dynamo_join_desc* D, int32_t T, const void* r, const vo
 
 }  // namespace
 
-extern "C" {
-
-dynamo_status dynamo_norm_join_forward(const dynamo_join_desc* desc, const void* r, const void* y, const void* w_post,
-                                       const void* gate, const void* w_pre, int32_t T, void* r_out, void* n_out, float* stats,
-                                       void* stream) {
+namespace dyn {
+// What dynamo_norm_join_forward refuses; dynamo_moe_block_forward asks before it launches the layer.
+dynamo_status check_join_forward(const dynamo_join_desc* desc, const void* r, const void* y, const void* w_post, const void* gate,
+                                      const void* w_pre, int32_t T, const void* r_out, const void* n_out, const float* stats) {
     if (const dynamo_status s = check_join(desc, T); s != DYNAMO_OK) return s;
     if (T == 0) return DYNAMO_OK;
     if (!y && !desc->pre_norm) return DYNAMO_ERR_ARG;   // nothing to do
@@ -517,6 +516,17 @@ dynamo_status dynamo_norm_join_forward(const dynamo_join_desc* desc, const void*
     if (!aligned16(r, y, r_out, n_out) || !aligned16(w_post, w_pre) ||
         (y && desc->gate_kind == DYNAMO_GATE_CHANNEL && !aligned16(gate)) || ((uintptr_t)stats & 7))
         return DYNAMO_ERR_ALIGN;
+    return DYNAMO_OK;
+}
+}  // namespace dyn
+
+extern "C" {
+
+dynamo_status dynamo_norm_join_forward(const dynamo_join_desc* desc, const void* r, const void* y, const void* w_post,
+                                       const void* gate, const void* w_pre, int32_t T, void* r_out, void* n_out, float* stats,
+                                       void* stream) {
+    if (const dynamo_status s = dyn::check_join_forward(desc, r, y, w_post, gate, w_pre, T, r_out, n_out, stats); s != DYNAMO_OK) return s;
+    if (T == 0) return DYNAMO_OK;
     int n_sms = 0;
     if (count_sms(&n_sms) != cudaSuccess) return DYNAMO_ERR_CUDA;
     JoinArgs a = join_args(desc, T, r, y, w_post, gate, w_pre);

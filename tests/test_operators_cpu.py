@@ -98,6 +98,27 @@ def test_norm_join_refusals(lib):
     assert bwd(y=None, dwp=None) == ARG and bwd(pre_norm=0, dwq=None, dro=None) == NULL
 
 
+def test_block_refusals(lib):
+    """What the layer refuses and what the join refuses, before either is launched; a layer without weights comes last."""
+    st, ctx = binding.dynamo_create(binding.LayerDesc(256, 512, 8, 0, 2, 64, 16, 16, 64, 1))
+    assert st == OK
+    good = dict(d=256, ydt=1, rdt=0, ndt=0, wdt=0, kind=0, post=1, pre=1, a=1.0, b=1.0, eps=1e-6, ctx=ctx, r=P, n=P, w=P, wp=P, gate=None, wq=P,
+                T=4, y=P, ro=P, no=P, st=None)
+
+    def call(desc=True, **kw):
+        a = {**good, **kw}
+        D = binding.JoinDesc(*(a[k] for k in ("d", "ydt", "rdt", "ndt", "wdt", "kind", "post", "pre", "a", "b", "eps")))
+        return lib.dynamo_moe_block_forward(a["ctx"], ctypes.byref(D) if desc else None, a["r"], a["n"], a["w"], None, a["wp"], a["gate"],
+                                            a["wq"], a["T"], a["y"], a["ro"], a["no"], a["st"], None, None)
+
+    for kw, want in ((dict(ctx=None), NULL), (dict(desc=False), NULL), (dict(d=264), SHAPE), (dict(y=None), NULL), (dict(r=None), NULL),
+                     (dict(ro=None), NULL), (dict(no=None), NULL), (dict(kind=1), NULL), (dict(kind=7), ARG), (dict(eps=0.0), ARG),
+                     (dict(a=float("inf")), ARG), (dict(ydt=5), SHAPE), (dict(wp=P + 2), ALIGN), (dict(st=P + 4), ALIGN), (dict(T=-1), TOKENS),
+                     (dict(), 9)):
+        assert call(**kw) == want, kw
+    assert binding.dynamo_destroy(ctx) == OK
+
+
 def test_linear_refusals(lib):
     def quant(w=P, N=8, K=128, G=64, c=P, p=P):
         return lib.dynamo_linear_quantize(w, N, K, G, c, p, None)
