@@ -14,7 +14,6 @@
 
 #include "../../include/dynamo.h"
 #include "common.cuh"
-#include "f32x2.cuh"
 #include "quant.cuh"
 #include "tcgen05.cuh"
 #include "vec8.cuh"
@@ -307,16 +306,18 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 //                  indices of codes at a time -> 16 + q as bf16 pairs -> A buffer (16x256b stores, so that four lanes read a
 //                  row's codes; a row a lane kept the L1 busy with 32 lines a load).  The codes come by cp.async, three jobs of a warp
 //                  on their way: 96 KB an SM (one job in registers left the loads' latency to bind)
-//   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + (m - 16 s) * sum(x), two columns an instruction;
-//                  sixteen warps at 64 tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 90.7 / 53.2 us;
-//                  eight warps 107 / 50.6; sixteen of a quarter of the columns and both row tiles, half the reads of the sums: 109 / 54.6)
+//   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + (m - 16 s) * sum(x); sixteen warps at 64
+//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 78.3 / 55.4 us; with packed pairs, whose moves
+//                  and registers cost more than the instructions they save, 85.1 / 54.1, and both halves of the columns on their way
+//                  90.0 / 53.7, spilling; eight warps 107 / 50.6; sixteen of a quarter of the columns and both row tiles, half the reads of
+//                  the sums, 109 / 54.6)
 //   next  fetch  : one thread; a bulk copy a stage of the activations, which linear_x_kernel has put into the operand's order,
 //                  with their sums per group behind them
 //   last  MMA    : 2 * 128 / 16 tcgen05.mma of 128 x TOK x 16 a stage, a run and one commit
 // Roles meet at barriers only, so that the chain of a stage (codes, expansion, MMAs, fold) overlaps its neighbours', blocks' ends
 // included; the same work by eight warps that all did every part, a barrier of the CTA a stage, took 88 us at 64 tokens, 14336 x 14336.
-// Bound by the fold at 64 tokens (2000 cycles a group's 256 x 64 results, two instructions a pair of them and the reads of accumulators and
-// sums), by the expansion and the hand-overs at 32 and fewer: 43.3 us, 39% of what the codes' bytes take.
+// Bound by the fold at 64 tokens (63% of the issue slots at groups of 64), by the expansion and the hand-overs at 32 and fewer:
+// 43.4 us at 14336 x 14336, 39% of what the codes' bytes take.
 // A block that lies within one CTA's run goes from the fold warps' registers to y; the pieces of the others go to the workspace, and a
 // kernel behind this one adds them up in the order of the CTAs.
 // Tensor memory: two A buffers of 128 columns, then BUFS accumulator buffers of 2 * TOK, one a group.
@@ -407,8 +408,9 @@ struct TcPos {
         tile = block / R.blocks;
         n0 = (block - tile * R.blocks) * TC_ROWS;
     }
-    __device__ __forceinline__ bool step(const TcRole& R) {   // true: to another block
-        if (++u < R.stages) return false;
+    __device__ __forceinline__ bool step(const TcRole& R, int by = 1) {   // true: to another block, its first stage
+        u += by;
+        if (u < R.stages) return false;
         u = 0;
         n0 += TC_ROWS;
         if (n0 == R.blocks * TC_ROWS) n0 = 0, ++tile;
@@ -424,6 +426,9 @@ __device__ __forceinline__ int stage_groups(int u, int K) {
     return G == LIN_UNIT ? 1 : min(LIN_UNIT / G, K / G - u * (LIN_UNIT / G));
 }
 
+__device__ __forceinline__ void lds64(uint32_t a, uint32_t& x, uint32_t& y) {
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(x), "=r"(y) : "r"(a) : "memory");
+}
 template <int G>
 __device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int warp, int lane) {
     using S = TcShape<64, G>;
@@ -433,14 +438,16 @@ __device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int w
     const int N = a.N, K = a.K;
     TcShared* const sh = R.S;
     const uint8_t* const base = a.codes;
-    const uint32_t mine = R.codes + warp * (TC_JOBS * 4096) + lane * 16;   // [job][atom][row half][lane] 16 bytes
+    // [job][atom][row half][row 8][64 bytes]; groups of 64: rows 2, 3, 6, 7 with their halves exchanged, for the banks of the 8-byte reads
+    const uint32_t ring = R.codes + warp * (TC_JOBS * 4096) + gid * 64, flip = G == LIN_UNIT ? 0 : gid & 2;
+    const uint32_t put = ring + 16 * (tid4 ^ flip), take = G == LIN_UNIT ? put : ring + 16 * ((tid4 >> 1) ^ flip) + 8 * (tid4 & 1);
     TcPos ahead(R);
     if (kh) ahead.step(R);
     int s_ahead = kh;
     uint32_t rows[4][2];   // byte offsets of the lane's rows 128 (i >> 1) + 32 q + 16 (i & 1) + gid (+ 8) in the block
     const uint8_t* from;   // of the block's first row, at the lane's place
     auto block_ahead = [&]() {
-        from = base + (long long)ahead.n0 * (K / 2) + tid4 * (4 * S::W);
+        from = base + (long long)ahead.n0 * (K / 2) + tid4 * 16;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -457,13 +464,8 @@ __device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int w
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const uint8_t* at = from + (rows[i][e] + k);
-                    const uint32_t to = mine + job * 4096 + i * 1024 + e * 512;
-                    if constexpr (G == LIN_UNIT) {
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(at) : "memory");
-                    } else {   // eight bytes of either group
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(at) : "memory");
-                        if (ng == 2) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to + 8), "l"(at + G / 2) : "memory");
-                    }
+                    if (G == LIN_UNIT || ng == 2 || tid4 < 2)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(put + job * 4096 + i * 1024 + e * 512), "l"(at) : "memory");
                 }
             s_ahead += 2;
             const bool a1 = ahead.step(R), a2 = ahead.step(R);
@@ -477,14 +479,25 @@ __device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int w
     uint32_t par = 1;   // of the round that emptied the A buffer before (passes at once the first time)
     for (int s = kh; s < R.n; s += 2, par ^= 1) {
         const uint32_t free = bar_test(TC_BAR(a_empty, kh), par);
-        asm volatile("cp.async.wait_group %0;" ::"n"(TC_JOBS - 1) : "memory");   // this job's codes (each lane its own)
+        asm volatile("cp.async.wait_group %0;" ::"n"(TC_JOBS - 1) : "memory");   // this job's codes 
+        __syncwarp();   // of all lanes
         if (!warp_saw(free) && !warp_wait(TC_BAR(a_empty, kh), par, &sh->poison, g_linear_status, 1, s)) break;
         tc_fence_after();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t to = R.tm + ((uint32_t)(32 * q + 16 * (i & 1)) << 16) + 128 * kh + 64 * (i >> 1);
-            const uint4 v0 = lds128(mine + job * 4096 + i * 1024), v1 = lds128(mine + job * 4096 + i * 1024 + 512);
-            const uint32_t cw[2][4] = {{v0.x, v0.y, v0.z, v0.w}, {v1.x, v1.y, v1.z, v1.w}};
+            uint32_t cw[2][4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t at = take + job * 4096 + i * 1024 + e * 512;
+                if constexpr (G == LIN_UNIT) {
+                    const uint4 v = lds128(at);
+                    cw[e][0] = v.x, cw[e][1] = v.y, cw[e][2] = v.z, cw[e][3] = v.w;
+                } else {   // eight bytes of either group
+                    lds64(at, cw[e][0], cw[e][1]);
+                    lds64(at ^ 32, cw[e][2], cw[e][3]);
+                }
+            }
             uint32_t r[32];   // words in pairs of columns: register 4 j + 2 e (+ 1) is row gid + 8 e, pairs 2 j, 2 j + 1
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -496,7 +509,8 @@ __device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int w
                 }
             tc_st_x8(to, r);
         }
-        bring(job);   // into the place of the codes that have just been stored
+        __syncwarp();
+        bring(job);   // into the place of the codes that have just been read
         job = job + 1 == TC_JOBS ? 0 : job + 1;
         tc_wait_st();
         tc_fence_before();
@@ -565,12 +579,13 @@ __device__ __noinline__ void tc_mma_role(const LinearArgs& a, TcRole R) {
     }
 }
 
-// Sixteen consecutive values that all lanes read, as pairs, asked for together.
-__device__ __forceinline__ void lds_pairs16(uint32_t a, F2 (&v)[8]) {
+// Sixteen consecutive values that all lanes read, asked for together.
+__device__ __forceinline__ void lds_values16(uint32_t a, float (&v)[16]) {
     asm volatile(
-        "ld.shared.v2.b64 {%0,%1}, [%8];\n\tld.shared.v2.b64 {%2,%3}, [%8+16];\n\t"
-        "ld.shared.v2.b64 {%4,%5}, [%8+32];\n\tld.shared.v2.b64 {%6,%7}, [%8+48];"
-        : "=l"(v[0].v), "=l"(v[1].v), "=l"(v[2].v), "=l"(v[3].v), "=l"(v[4].v), "=l"(v[5].v), "=l"(v[6].v), "=l"(v[7].v)
+        "ld.shared.v4.f32 {%0,%1,%2,%3}, [%16];\n\tld.shared.v4.f32 {%4,%5,%6,%7}, [%16+16];\n\t"
+        "ld.shared.v4.f32 {%8,%9,%10,%11}, [%16+32];\n\tld.shared.v4.f32 {%12,%13,%14,%15}, [%16+48];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+          "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
         : "r"(a)
         : "memory");
 }
@@ -582,47 +597,63 @@ __device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw,
     const int K = a.K, N = a.N, groups = K / G, row_in = 128 * mt + 32 * q + lane;
     const uint32_t* const params = a.params;
     TcShared* const sh = R.S;
-    F2 total[NC / 2];
+    float total[NC];
 #pragma unroll
-    for (int c = 0; c < NC / 2; ++c) total[c] = f2(0.f);
+    for (int c = 0; c < NC; ++c) total[c] = 0.f;
+    // Parameters, four groups of the lane's row at a time and one load ahead: a load takes the L1 a pass per row, and one by one these
+    // were 40% of its passes.
+    constexpr int QUAD = 4 / S::GROUPS;   // stages
     TcPos pos(R), ahead(R);
-    const uint32_t* from;   // parameters of the lane's row in the block ahead
+    const uint32_t* from;   // of the block ahead
     auto block_ahead = [&]() { from = params + (long long)min(ahead.n0 + row_in, N - 1) * groups; };
     block_ahead();
-    uint32_t pr[S::GROUPS];
-    auto load_params = [&]() {   // of the stage `ahead`
-#pragma unroll
-        for (int g = 0; g < S::GROUPS; ++g) pr[g] = g < stage_groups<G>(ahead.u, K) ? __ldg(from + ahead.u * S::GROUPS + g) : 0u;
-        if (ahead.step(R)) block_ahead();
+    uint4 cur, nxt;
+    int left = 0;           // stages that cur has left
+    auto load_quad = [&]() {
+        const int g = ahead.u * S::GROUPS & ~3;
+        if ((groups & 3) == 0)
+            nxt = __ldg(reinterpret_cast<const uint4*>(from + g));
+        else
+            nxt = make_uint4(__ldg(from + g), g + 1 < groups ? __ldg(from + g + 1) : 0u, g + 2 < groups ? __ldg(from + g + 2) : 0u,
+                             g + 3 < groups ? __ldg(from + g + 3) : 0u);
+        if (ahead.step(R, QUAD - ahead.u % QUAD)) block_ahead();
     };
-    if (R.n > 0) load_params();
+    load_quad();
     bool ok = true;
     uint32_t buf = 0, par = 0, ready = 0;
     const int u_first = pos.u;   // a first block that does not begin with its first stage is a piece
     int piece = 0;
     for (int s = 0; s < R.n; ++s) {
         const int slot = s % TC_SLOTS, ng = stage_groups<G>(pos.u, K);
+        if (left == 0) {
+            cur = nxt;
+            const int skip = pos.u % QUAD;
+            left = min(QUAD - skip, R.stages - pos.u);
+            if (skip * S::GROUPS & 1) cur.x = cur.y, cur.y = cur.z, cur.z = cur.w;
+            if (skip * S::GROUPS & 2) cur.x = cur.z, cur.y = cur.w;
+            load_quad();
+        }
+        --left;
         float s1[S::GROUPS], m1[S::GROUPS];
 #pragma unroll
         for (int g = 0; g < S::GROUPS; ++g) {
-            const __half2 pv = *reinterpret_cast<const __half2*>(&pr[g]);
+            const __half2 pv = *reinterpret_cast<const __half2*>(&cur.x);
             s1[g] = __low2float(pv);
             m1[g] = fmaf(-16.f, s1[g], __high2float(pv));
+            cur.x = cur.y, cur.y = cur.z, cur.z = cur.w;
         }
-        if (s + 1 < R.n) load_params();
         if (ok) ok = warp_saw(ready) || warp_wait(TC_BAR(x_full, slot), (s / TC_SLOTS) & 1, &sh->poison, g_linear_status, 5, s);
         uint32_t full = bar_test(TC_BAR(acc_full, buf), par);
         ready = bar_test(TC_BAR(x_full, (s + 1) % TC_SLOTS), ((s + 1) / TC_SLOTS) & 1);
         // zero-points times the sums, as soon as the copies have landed (a group that is not there: m = 0, sums of zeros)
 #pragma unroll
         for (int g = 0; g < S::GROUPS; ++g) {
-            const F2 m2 = f2(m1[g]);
 #pragma unroll
             for (int c0 = 0; c0 < NC; c0 += 16) {
-                F2 x[8];
-                lds_pairs16(R.ring + slot * S::XB + 16 * S::LBO + (g * TOK + col0 + c0) * 4, x);
+                float x[16];
+                lds_values16(R.ring + slot * S::XB + 16 * S::LBO + (g * TOK + col0 + c0) * 4, x);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) total[c0 / 2 + c] = fma2(m2, x[c], total[c0 / 2 + c]);
+                for (int c = 0; c < 16; ++c) total[c0 + c] = fmaf(m1[g], x[c], total[c0 + c]);
             }
         }
         __syncwarp();
@@ -634,21 +665,16 @@ __device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw,
             if (!ok) break;
             tc_fence_after();
             const uint32_t acc = R.tm + ((uint32_t)(32 * q) << 16) + 256 + buf * (2 * TOK) + mt * TOK + col0;
-            const F2 sg = f2(s1[g]);
-            uint32_t r[2][16];
-            tc_ld_rows16(acc, r[0]);
-#pragma unroll
-            for (int c0 = 0; c0 < NC; c0 += 16) {
-                uint32_t(&rr)[16] = r[(c0 / 16) & 1];
+            auto sixteen = [&](const int c0) {
+                uint32_t rr[16];
+                tc_ld_rows16(acc + c0, rr);
                 // (with the registers: what is read of them stays behind the wait)
                 asm volatile("tcgen05.wait::ld.sync.aligned;"
                              : "+r"(rr[0]), "+r"(rr[1]), "+r"(rr[2]), "+r"(rr[3]), "+r"(rr[4]), "+r"(rr[5]), "+r"(rr[6]), "+r"(rr[7]), "+r"(rr[8]),
                                "+r"(rr[9]), "+r"(rr[10]), "+r"(rr[11]), "+r"(rr[12]), "+r"(rr[13]), "+r"(rr[14]), "+r"(rr[15])
                              :
                              : "memory");
-                if (c0 + 16 < NC) {
-                    tc_ld_rows16(acc + c0 + 16, r[(c0 / 16 + 1) & 1]);
-                } else {   // the buffer is read: hand it back
+                if (c0 + 16 >= NC) {   // the buffer is read: hand it back
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive(TC_BAR(acc_empty, buf));
@@ -656,9 +682,10 @@ __device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw,
                     if (g + 1 < ng) full = bar_test(TC_BAR(acc_full, buf), par);
                 }
 #pragma unroll
-                for (int c = 0; c < 16; c += 2)
-                    total[(c0 + c) / 2] = fma2(sg, f2(__uint_as_float(rr[c]), __uint_as_float(rr[c + 1])), total[(c0 + c) / 2]);
-            }
+                for (int c = 0; c < 16; ++c) total[c0 + c] = fmaf(s1[g], __uint_as_float(rr[c]), total[c0 + c]);
+            };
+#pragma unroll
+            for (int c0 = 0; c0 < NC; c0 += 16) sixteen(c0);
         }
         if (pos.u + 1 == R.stages || s + 1 == R.n) {
             // the block's end, or the run's: a row a lane, so a column's stores of a warp are 32 consecutive values
@@ -667,12 +694,12 @@ __device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw,
             float* part = a.part + ((long long)(2 * blockIdx.x + (piece ? 1 : 0)) * TOK + col0) * TC_ROWS + row_in;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const float v = !ok ? __int_as_float(0x7fffffff) : c & 1 ? hi(total[c / 2]) : lo(total[c / 2]);
+                const float v = !ok ? __int_as_float(0x7fffffff) : total[c];
                 if (!whole) part[c * TC_ROWS] = v;
                 else store_y<TO>(a, t0 + c, row, v);
             }
 #pragma unroll
-            for (int c = 0; c < NC / 2; ++c) total[c] = f2(0.f);
+            for (int c = 0; c < NC; ++c) total[c] = 0.f;
             piece = 1;
         }
         pos.step(R);
