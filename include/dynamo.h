@@ -389,7 +389,7 @@ dynamo_status dynamo_route_permute_static(const float* router_logits, int32_t T,
  * floating-point atomics).  Row-major contiguous arrays, 16-byte aligned (ERR_ALIGN); a *_dtype is DYNAMO_BF16 or
  * DYNAMO_F32 (ERR_SHAPE otherwise); widths are multiples of 8 (ERR_SHAPE).  Outputs must not overlap inputs or one
  * another unless stated.  Sums, norms and weights are worked out in fp32, results rounded once.  T = 0 is a no-op unless
- * stated.
+ * stated.  A workspace is one call's from its launch to its end: calls or graphs that may run at the same time need one each.
  *
  * Tokens sorted by expert and back (Section II-A: one-to-many dispatch; for experts other than the layer's own, and for
  * training what stands around them).
