@@ -76,6 +76,15 @@ __device__ __forceinline__ void store8(T* p, const F2 (&v)[4]) {
     store8(p, f);
 }
 
+// Eight columns that are read twice: by loads that the compiler may not merge with the first ones (the values would stay in registers).
+__device__ __forceinline__ uint4 reread16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ Raw8<__nv_bfloat16> reread8(const __nv_bfloat16* p) { return {reread16(p)}; }
+__device__ __forceinline__ Raw8<float> reread8(const float* p) { return {reread16(p), reread16(p + 4)}; }
+
 // Sum of a value over the TPR threads of a row; every thread gets it.  `scratch`: [TPR / 32], two of them in turn.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* scratch) {
@@ -128,7 +137,7 @@ __host__ __device__ constexpr int ctas_of(int threads, int regs) { return 65536 
 // a half times as many registers, 96, 25.1 against 24.7 us, fewer, 42, 34), one in the backward one (64 registers 70 us
 // against 42.9).  Two runs a thread instead: forward 25.1, backward 65 us at 128 registers, 44 at 168.
 __host__ __device__ constexpr int join_regs() { return 64; }
-__host__ __device__ constexpr int grad_regs(int tpr) { return tpr == 1024 ? 64 : 128; }
+__host__ __device__ constexpr int grad_regs() { return 128; }
 
 // What a column needs of the weights: the post-norm's times the channel's gate, and the pre-norm's.
 __device__ __forceinline__ void post_weights(const JoinArgs& a, int c, F2 (&p)[4]) {
@@ -145,12 +154,19 @@ __device__ __forceinline__ void pre_weights(const JoinArgs& a, int c, F2 (&q)[4]
     for (int j = 0; j < 4; ++j) q[j] = f2(w[2 * j], w[2 * j + 1]);
 }
 
+// Asks for a thread's eight columns of a row that is read later; a line is asked for by the thread whose piece begins it.
+template <typename T>
+__device__ __forceinline__ void ask_for(const T* p) {
+    if (((uintptr_t)p & 127) < 8 * sizeof(T)) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
+
 // TPR threads a row, V runs of eight columns a thread (run i of thread t: columns 8 (t + i TPR)).  The CTAs that the SMs hold walk
 // the rows, each thread with its columns' weights in registers and the next row on its way while it works on the present one.
 // What bounds it is instructions as much as memory: two columns an instruction (f32x2).  4096 rows of 4096, bf16, gate per
 // channel: 24.7 us, 5.4 TB/s of rows; 36.7 with a CTA a row that read the weights for it (half as many bytes again as the
 // row's), 30.9 with one column an instruction.
-// KEEP = false (rows too wide for that): weights and rows are read when they are used.
+// KEEP = false (rows too wide for that): weights and rows are read when they are used, the next row asked for ahead (1024 rows of 16384,
+// bf16: 33.2 us; 36.4 without).
 template <typename TY, typename TR, int TPR, int V, bool KEEP>
 __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), join_regs()))
     norm_join_kernel(const __grid_constant__ JoinArgs a) {
@@ -197,6 +213,14 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), join
         }
         const float gate = a.block_scale * R.gt;
         if constexpr (KEEP) fetch(R, t + step);   // on its way from here on, into the registers that were just read
+        else if (t + step < a.T)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int c = 8 * (tt + i * TPR);
+                if (c >= d) continue;
+                if (a.y) ask_for((const TY*)a.y + (t + step) * d + c);
+                ask_for((const TR*)a.r + (t + step) * d + c);
+            }
         float s_y = 1.f;
         if (a.post) {
             F2 sum2 = f2(0.f);
@@ -249,7 +273,7 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), join
 // copy of the row that came, 56 with the rows staged in shared memory and read twice.  The column sums of d_w_post and of a channel gate differ by a factor of the column
 // (S1 = sum_t block_scale gate_t G y s_y; d_w_post = gate S1, d_gate = w_post S1), so that two sums a column are kept.
 template <typename TY, typename TR, typename TN, int TPR, int V, bool KEEP>
-__global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), grad_regs(TPR)))
+__global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), grad_regs()))
     norm_join_grad_kernel(const __grid_constant__ JoinArgs a) {
     constexpr int THREADS = threads_of(TPR), ROWS = THREADS / TPR, W = TPR / 32;
     __shared__ float scratch[2][4 * W];
@@ -395,6 +419,121 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), grad
     }
 }
 
+// Eight column sums, in two halves `apart` from one another.
+__device__ __forceinline__ void take8(const float4* at, int apart, F2 (&v)[4]) {
+    const float4 x = at[0], y = at[apart];
+    v[0] = f2(x.x, x.y), v[1] = f2(x.z, x.w), v[2] = f2(y.x, y.y), v[3] = f2(y.z, y.w);
+}
+__device__ __forceinline__ void give8(float4* at, int apart, const F2 (&v)[4]) {
+    at[0] = make_float4(lo(v[0]), hi(v[0]), lo(v[1]), hi(v[1]));
+    at[apart] = make_float4(lo(v[2]), hi(v[2]), lo(v[3]), hi(v[3]));
+}
+// The gradient of rows too wide for a thread's registers to hold: the first pass keeps the sums alone, the second reads the row again
+// (from the L1 or L2; the next row is asked for meanwhile) and works the same values out again.  The weights are read when they
+// are used; the column sums stand in shared memory, a thread's own columns: [sum][half][run][4].
+constexpr int WIDE_THREADS = 512;
+template <typename TY, typename TR, typename TN>
+__global__ void __launch_bounds__(WIDE_THREADS, 1) norm_join_grad_wide_kernel(const __grid_constant__ JoinArgs a) {
+    constexpr int TPR = WIDE_THREADS;
+    __shared__ float scratch[2][4 * TPR / 32];
+    extern __shared__ __align__(16) float s_sum[];
+    pdl_prologue();
+    const int tt = threadIdx.x, d = a.d;
+    const float inv_d = 1.f / (float)d;
+    const F2 res = f2(a.y ? a.res_scale : 1.f);
+    const int runs = d / 8;
+    float4* const sums = reinterpret_cast<float4*>(s_sum);
+    if (a.part)
+        for (int i = tt; i < runs; i += TPR)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) sums[h * runs + i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    int turn = 0;
+    for (long long t = blockIdx.x; t < a.T; t += gridDim.x, turn ^= 1) {
+        const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * t);
+        const float s_y = a.post ? st.x : 1.f, s_r = st.y;
+        const float gz = a.block_scale * (a.gate_kind == DYNAMO_GATE_TOKEN ? ((const float*)a.gate)[t] : 1.f);
+        const F2 gy2 = f2(gz * s_y), sr2 = f2(s_r);
+        // y, dn, r' (x), dr' + s_r u (g), u and p y of eight columns
+        struct Columns {
+            F2 p[4], y[4], dn[4], x[4], g[4], u[4], py[4];
+        };
+        auto columns = [&](Columns& C, int c) {
+            const long long at = t * d + c;
+            F2 q[4];
+            unpack8(a.y ? reread8((const TY*)a.y + at) : zero8<TY>(), C.y);
+            unpack8(reread8((const TR*)a.r + at), C.x);
+            unpack8(a.d_r_out ? reread8((const TR*)a.d_r_out + at) : zero8<TR>(), C.g);
+            unpack8(a.d_n ? reread8((const TN*)a.d_n + at) : zero8<TN>(), C.dn);
+            post_weights(a, c, C.p);
+            pre_weights(a, c, q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                C.py[j] = mul2(C.p[j], C.y[j]);
+                C.x[j] = fma2(gy2, C.py[j], mul2(res, C.x[j]));
+                C.u[j] = mul2(q[j], C.dn[j]);
+                C.g[j] = fma2(sr2, C.u[j], C.g[j]);
+            }
+        };
+        F2 sum2[3] = {f2(0.f), f2(0.f), f2(0.f)};   // as in norm_join_grad_kernel
+#pragma unroll 2
+        for (int i = tt; i < runs; i += TPR) {
+            const int c = 8 * i;
+            Columns C;
+            columns(C, c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sum2[0] = fma2(C.u[j], C.x[j], sum2[0]);
+                sum2[1] = fma2(C.py[j], C.g[j], sum2[1]);
+                sum2[2] = fma2(C.py[j], C.x[j], sum2[2]);
+            }
+            const long long next = (t + gridDim.x) * d + c;
+            if (t + gridDim.x < a.T) {
+                if (a.y) ask_for((const TY*)a.y + next);
+                ask_for((const TR*)a.r + next);
+                if (a.d_r_out) ask_for((const TR*)a.d_r_out + next);
+                if (a.d_n) ask_for((const TN*)a.d_n + next);
+            }
+        }
+        float sum[3] = {lo(sum2[0]) + hi(sum2[0]), lo(sum2[1]) + hi(sum2[1]), lo(sum2[2]) + hi(sum2[2])};
+        row_sums<TPR>(sum, scratch[turn]);
+        const float ca = s_r * s_r * s_r * inv_d * sum[0], zg = s_y * (sum[1] - ca * sum[2]);
+        if (a.d_gate && a.gate_kind == DYNAMO_GATE_TOKEN && tt == 0) a.d_gate[t] = a.block_scale * zg;
+        const float cv = a.post ? gz * zg * inv_d : 0.f;
+        const F2 ca2 = f2(-ca), cy2 = f2(-cv * s_y * s_y);
+#pragma unroll 2
+        for (int i = tt; i < runs; i += TPR) {
+            const int c = 8 * i;
+            Columns C;
+            columns(C, c);
+            F2 s1[4] = {f2(0.f), f2(0.f), f2(0.f), f2(0.f)}, s2[4] = {s1[0], s1[0], s1[0], s1[0]};
+            if (a.part) {
+                take8(sums + i, runs, s1);
+                take8(sums + 2 * runs + i, runs, s2);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const F2 G = fma2(ca2, C.x[j], C.g[j]);
+                const F2 gG = mul2(gy2, G);
+                s1[j] = fma2(gG, C.y[j], s1[j]);
+                s2[j] = fma2(C.dn[j], mul2(C.x[j], sr2), s2[j]);
+                C.y[j] = fma2(C.p[j], gG, mul2(cy2, C.y[j]));
+                C.g[j] = mul2(res, G);
+            }
+            if (a.part) {
+                give8(sums + i, runs, s1);
+                give8(sums + 2 * runs + i, runs, s2);
+            }
+            if (a.d_r) store8((TR*)a.d_r + t * d + c, C.g);
+            if (a.d_y) store8((TY*)a.d_y + t * d + c, C.y);
+        }
+    }
+    if (!a.part) return;
+    float* part = a.part + (long long)blockIdx.x * 2 * d;
+    for (int i = tt; i < runs; i += TPR)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) *reinterpret_cast<float4*>(part + (h >> 1) * d + 8 * i + 4 * (h & 1)) = sums[h * runs + i];
+}
+
 // Column sums of the CTAs' partial rows, in a fixed order, and the factors of the two gradients that share one.  grid.y: which
 // of the two sums.
 __global__ void __launch_bounds__(1024) norm_join_sums_kernel(const __grid_constant__ JoinArgs a, int n_part, float* d_w_post,
@@ -423,7 +562,9 @@ __global__ void __launch_bounds__(1024) norm_join_sums_kernel(const __grid_const
 constexpr int JOIN_MAX_D = 16384;
 
 // Threads a row and runs a thread by the width: a run a thread as far as registers allow, one warp a row (no barrier) while
-// that is enough.
+// that is enough.  The gradient of rows above 8192 has a kernel that keeps no row (V = 0): 1024 rows of 12288 / 16384 bf16 59 / 80 us, 85 / 112
+// with two runs in 64 registers of 1024 threads; below, two runs in 128 registers of 512 are faster (2048 rows of 5000 / 8192: 49 / 60 us,
+// 70 / 71 without keeping the row).
 template <int TPR_, int V_, bool KEEP_>
 struct Layout {
     static constexpr int TPR = TPR_, V = V_;
@@ -436,11 +577,8 @@ static cudaError_t by_width(int d, F f) {
     if (d <= 1024) return f(Layout<128, 1, true>{});
     if (d <= 2048) return f(Layout<256, 1, true>{});
     if (d <= 4096) return f(Layout<512, 1, true>{});
-    if (d <= 8192) {
-        if constexpr (GRAD) return f(Layout<512, 2, false>{});
-        else return f(Layout<1024, 1, true>{});
-    }
-    return f(Layout<1024, 2, false>{});
+    if constexpr (GRAD) return d <= 8192 ? f(Layout<512, 2, false>{}) : f(Layout<WIDE_THREADS, 0, false>{});
+    else return d <= 8192 ? f(Layout<1024, 1, true>{}) : f(Layout<1024, 2, false>{});
 }
 template <typename F>
 static cudaError_t by_types(int a, int b, F f) {
@@ -457,7 +595,7 @@ static int grad_ctas(int T, int d, int n_sms) {
     int n = 0;
     by_width<true>(d, [&](auto l) {
         constexpr int TPR = decltype(l)::TPR;
-        n = join_ctas(T, TPR, ctas_of(threads_of(TPR), grad_regs(TPR)), n_sms);
+        n = join_ctas(T, TPR, ctas_of(threads_of(TPR), grad_regs()), n_sms);
         return cudaSuccess;
     });
     return n;
@@ -592,8 +730,17 @@ dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void
             using L = decltype(l);
             const dim3 grid((unsigned)ctas), block(threads_of(L::TPR));
             const size_t smem = threads_of(L::TPR) > L::TPR ? 2 * desc->d * sizeof(float) : 0;
-            return a.n_f32 ? launch_pdl(norm_join_grad_kernel<TY, TR, float, L::TPR, L::V, L::KEEP>, grid, block, smem, st, a)
-                           : launch_pdl(norm_join_grad_kernel<TY, TR, __nv_bfloat16, L::TPR, L::V, L::KEEP>, grid, block, smem, st, a);
+            if constexpr (L::V == 0) {
+                auto wide = [&](auto kernel) {
+                    const size_t sums = a.part ? 2 * (size_t)desc->d * sizeof(float) : 0;
+                    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sums);
+                    return e != cudaSuccess ? e : launch_pdl(kernel, grid, block, sums, st, a);
+                };
+                return a.n_f32 ? wide(norm_join_grad_wide_kernel<TY, TR, float>) : wide(norm_join_grad_wide_kernel<TY, TR, __nv_bfloat16>);
+            } else {
+                return a.n_f32 ? launch_pdl(norm_join_grad_kernel<TY, TR, float, L::TPR, L::V, L::KEEP>, grid, block, smem, st, a)
+                               : launch_pdl(norm_join_grad_kernel<TY, TR, __nv_bfloat16, L::TPR, L::V, L::KEEP>, grid, block, smem, st, a);
+            }
         });
     });
     if (e != cudaSuccess) return DYNAMO_ERR_CUDA;
