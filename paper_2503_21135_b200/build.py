@@ -100,7 +100,7 @@ def build_native(force: bool = False) -> str:
         torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
         cmd = ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
                 f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"] + [f"-isystem{p}" for p in include] +
-               ["-o", NATIVE, os.path.join(CSRC, NATIVE_SOURCE), f"-L{HERE}", "-l:libdynamo.so", f"-L{torch_lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu",
+               ["-o", NATIVE, os.path.join(CSRC, NATIVE_SOURCE), f"-L{HERE}", "-l:libdynamo.so", f"-L{torch_lib}", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda",
                 "-ltorch_python", "-Wl,-rpath,$ORIGIN"])
         subprocess.check_call(cmd)
         with open(manifest_path, "w") as f:
