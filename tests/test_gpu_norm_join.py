@@ -67,7 +67,7 @@ def reference(r, y, how):
 
 
 WIDTHS = [8, 64, 256, 264, 512, 520, 1024, 1408, 2048, 4096, 4104, 8192, 16384]
-CASES = [(T, d) for d in WIDTHS for T in (1, 5)] + [(0, 64), (3000, 64), (1500, 264), (1300, 1024), (700, 4096), (300, 8200)]
+CASES = [(T, d) for d in WIDTHS for T in (1, 5)] + [(0, 64), (3000, 64), (1500, 264), (1300, 1024), (700, 4096), (300, 8200), (450, 12296)]
 OPTIONS = [("bf16", "bf16", "f32", "channel", "weight", "weight", "bf16"), ("f32", "f32", "bf16", "token", "weight", "weight", "f32"),
            ("f32", "bf16", "f32", "none", "ones", "ones", "bf16"), ("bf16", "f32", "bf16", "channel", "off", "weight", "bf16"),
            ("bf16", "bf16", "bf16", "token", "weight", "off", "bf16")]
