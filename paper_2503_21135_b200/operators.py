@@ -105,3 +105,9 @@ def linear(x: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, y_dtype: 
            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [T, N] = x bf16 [T, K] times the transposed matrix that codes and params stand for."""
     return _lib().linear(x, codes, params, y_dtype, out)
+
+
+def poll_linear_status() -> int:
+    """Waits for the current stream.  0, or the library's ERR_TIMEOUT if a bounded wait of ``linear`` has expired on the current
+    device since the last call: results of that time that are NaN are lost."""
+    return load().dynamo_linear_poll_status(torch.cuda.current_stream().cuda_stream)

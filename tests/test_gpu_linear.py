@@ -77,7 +77,7 @@ def test_linear_many(T, N, K, G, y_dtype):
     codes, params = ops.quantize_linear(w, G)
     guard = torch.full((T + 1, N), 5.0, dtype=torch.float32 if y_dtype == "f32" else torch.bfloat16, device="cuda")
     y = ops.linear(x, codes, params, y_dtype=binding.F32 if y_dtype == "f32" else binding.BF16, out=guard[:T])
-    assert binding.load().dynamo_linear_poll_status(None) == 0
+    assert ops.poll_linear_status() == 0
     q = torch.stack([codes & 15, codes >> 4], 2).view(N, K).double()
     s, m = params.double().repeat_interleave(G, 1).unbind(2)
     X = x.double()
