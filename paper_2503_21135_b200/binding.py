@@ -399,7 +399,8 @@ class DynamoLayer:
         if gate is not None and not per_token:
             rows.append(gate)
         given = [r, n, w_router] + [t for t in (bias, w_post, gate, w_pre, y) if t is not None]
-        assert all(t.is_cuda and t.is_contiguous() and t.device == self.workspace.device for t in given)
+        device = r.device if self.workspace is None else self.workspace.device   # (no weights yet: the call itself refuses)
+        assert all(t.is_cuda and t.is_contiguous() and t.device == device for t in given)
         assert d == self.desc.d_model and r.dtype in types and n.shape == r.shape and n.dtype == torch.bfloat16
         assert tuple(w_router.shape) == (self.desc.n_experts, d) and w_router.dtype == torch.bfloat16
         assert bias is None or (bias.dtype == torch.float32 and bias.numel() == self.desc.n_experts)

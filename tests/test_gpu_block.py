@@ -92,6 +92,9 @@ def test_block_refusals(layer):
               lambda: gpu.forward_block(r, n, w_r, bias, gate=how["w_post"][:, None]), lambda: gpu.forward_block(r, n, w_r, bias, post_norm=False, w_post=how["w_post"])):
         with pytest.raises(AssertionError):
             f()
+    empty = binding.DynamoLayer.from_config(CFG, max_tokens=8)
+    with pytest.raises(binding.DynamoError):
+        empty.forward_block(r, n, w_r, bias)             # a layer without weights
     big, _ = stream(300, torch.bfloat16, "none")
     with pytest.raises(binding.DynamoError):
         gpu.forward_block(big, big.clone(), w_r, bias)   # more tokens than the layer has room for
