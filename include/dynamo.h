@@ -464,9 +464,10 @@ dynamo_status dynamo_moe_block_forward(dynamo_ctx* ctx, const dynamo_join_desc* 
  * dynamo_linear_quantize: w bf16 [rows, cols] -> codes uint8 [rows, cols / 2] (index 2i in the low, 2i + 1 in the high half of
  *   byte i) and params fp16 [rows, cols / G, 2] {scale, zero}, by the rule of dynamo_pack_experts at 4 bits.
  * dynamo_linear_forward: y[t][n] = sum_k (scale[n][k/G] * code[n][k] + zero[n][k/G]) * x[t][k]
- *   x bf16 [T, cols], y [T, rows] of y_dtype.  Products are exact, sums in fp32.  Made for the few rows of a decode step:
- *   large matrices are read once per 64 tokens, small ones (16 tokens x the matrix up to 3 * 2^24) per 16.  An infinite or NaN activation makes its row NaN; the sum of 31 |x| over a group
- *   has to stay in the range of fp32.
+ *   x bf16 [T, cols], y [T, rows] of y_dtype.  Products are exact, sums in fp32; a group whose codes are all 0 adds zero times its
+ *   activations' sum and nothing else (a row of zeros gives 0).  Made for the few rows of a decode step: large matrices are read
+ *   once per 64 tokens, small ones (16 tokens x the matrix up to 3 * 2^24) per 16.  A NaN activation makes its token's row NaN, an
+ *   infinite one makes it infinite or NaN; the sum of 31 |x| over a group has to stay in the range of fp32.
  *   workspace: dynamo_linear_workspace_bytes (0 for up to 8 tokens and small matrices: then it may be NULL), 256-byte aligned.
  * dynamo_linear_poll_status: synchronises the stream; DYNAMO_ERR_TIMEOUT if a bounded wait of dynamo_linear_forward expired on the
  *   current device since the last call (the results concerned are NaN), else DYNAMO_OK.

@@ -4,8 +4,10 @@
 //
 // The codes are row-major, two a byte (index 2i in the low half of byte i), so a 32-bit word holds eight consecutive ones.
 // A code becomes a bf16 operand by a shift, a mask and an OR: on the four highest mantissa bits of 16.0 it reads as
-// 16 + q, exactly.  The MMA therefore gives sum((16 + q) x), and 16 s goes off the zero-point:
-// y += s * acc + (m - 16 s) * sum(x), with sum(x) from an MMA whose other operand is ones.  Products are exact in fp32 (bf16 by
+// 16 + q, exactly; the 16 goes off again, either in the operand (one subtraction a pair, exact: the tcgen05 kernel) or off the
+// group's sum (the few-token kernel: sum((16 + q) x) - 16 sum(x), the second from MMAs with ones in the same steps, so that
+// the two cancel to 0 where the codes are 0).  Then y += s * sum(q x) + m * sum(x).  The zero-point is used as it is: a group of one value has
+// scale 1 and codes 0, and m - 16 s would lose an m that is small beside 16.  Products are exact in fp32 (bf16 by
 // bf16); sums, scales and zero-points are in fp32, y is rounded once.  The order in which a warp's 16-wide steps take the
 // input indices is free as long as codes and activations agree: a lane takes runs of consecutive ones from both.
 #include <algorithm>
@@ -60,7 +62,8 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 // Codes i and i + 4 of a word as the bf16 pair 16 + q.  The mask (0x0078 twice) and the pattern of 16.0 come with the kernel's
 // arguments: as constants that the compiler knows they became two logical instructions a pair, with an immediate each.
 struct PairBits {
-    uint32_t mask, sixteen;
+    uint32_t mask, sixteen;        // 0x0078 and 16.0, twice
+    uint32_t low, onetwentyeight;  // 0x000f and 128.0: a code on the four lowest mantissa bits of 128.0 reads as 128 + q
 };
 template <int I>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w, const PairBits& p) {
@@ -68,6 +71,17 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w, const PairBits& p) {
     uint32_t r;
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(s), "r"(p.mask), "r"(p.sixteen));   // (s & mask) | sixteen
     return r;
+}
+
+// The same pair as q itself, and two shifts for the four pairs of a word (w8 = w >> 8).
+template <int I>
+__device__ __forceinline__ uint32_t whole_pair(uint32_t w, uint32_t w8, const PairBits& p) {
+    const uint32_t s = I == 0 ? w : I == 1 ? w >> 1 : I == 2 ? w8 : w8 >> 1;
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(s), "r"(I & 1 ? p.mask : p.low), "r"(I & 1 ? p.sixteen : p.onetwentyeight));
+    const uint32_t off = I & 1 ? 0x41804180u : 0x43004300u;
+    const __nv_bfloat162 q = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&r), *reinterpret_cast<const __nv_bfloat162*>(&off));
+    return *reinterpret_cast<const uint32_t*>(&q);
 }
 
 struct LinearArgs {
@@ -162,7 +176,7 @@ __device__ __forceinline__ void sum_mmas(float (&sx)[4], const uint32_t (&b)[4])
     mma_bf16(sx, BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, b[0], b[1]);
     mma_bf16(sx, BF16_ONES, BF16_ONES, BF16_ONES, BF16_ONES, b[2], b[3]);
 }
-// A group's sums into the results: y += s * sum((16 + q) x) + (m - 16 s) * sum(x).
+// A group's sums into the results: y += s * (sum((16 + q) x) - 16 sum(x)) + m * sum(x).
 template <int NT>
 __device__ __forceinline__ void fold_group(float (&acc)[NT][4], const float (&c)[NT][4], const float (&sx)[NT][2], uint32_t pr0,
                                            uint32_t pr1) {
@@ -170,11 +184,12 @@ __device__ __forceinline__ void fold_group(float (&acc)[NT][4], const float (&c)
     for (int h = 0; h < 2; ++h) {
         const uint32_t pw = h ? pr1 : pr0;
         const __half2 pv = *reinterpret_cast<const __half2*>(&pw);
-        const float s = __low2float(pv), m = fmaf(-16.f, s, __high2float(pv));
+        const float s = __low2float(pv), m = __high2float(pv);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) acc[n][2 * h + i] = fmaf(s, c[n][2 * h + i], fmaf(m, sx[n][i], acc[n][2 * h + i]));
+            for (int i = 0; i < 2; ++i)
+                acc[n][2 * h + i] = fmaf(s, fmaf(-16.f, sx[n][i], c[n][2 * h + i]), fmaf(m, sx[n][i], acc[n][2 * h + i]));
     }
 }
 template <int NT>
@@ -303,12 +318,13 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 // The work is a line of stages: 256 rows (two row tiles of an MMA's 128) x 128 input indices for TOK tokens, a block's stages one behind
 // another; one persistent CTA per SM takes an equal run of it.  Roles by warp:
 //   0-7   expand : two groups of four (a warp per lane quarter of the tensor memory); a group takes every other stage: 16 rows x 128
-//                  indices of codes at a time -> 16 + q as bf16 pairs -> A buffer (16x256b stores, so that four lanes read a
+//                  indices of codes at a time -> q as bf16 pairs -> A buffer (16x256b stores, so that four lanes read a
 //                  row's codes; a row a lane kept the L1 busy with 32 lines a load).  The codes come by cp.async, three jobs of a warp
 //                  on their way: 96 KB an SM (one job in registers left the loads' latency to bind)
-//   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + (m - 16 s) * sum(x); sixteen warps at 64
-//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 78.3 / 55.4 us; with packed pairs, whose moves
-//                  and registers cost more than the instructions they save, 85.1 / 54.1, and both halves of the columns on their way
+//   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + m * sum(x); sixteen warps at 64
+//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 81.4 / 56.6 us; as 78.3 / 55.4 they were compared, before the
+//                  operand's 16 went off in the expansion, with packed pairs, whose moves and registers cost more than the instructions
+//                  they save, 85.1 / 54.1, and both halves of the columns on their way
 //                  90.0 / 53.7, spilling; eight warps 107 / 50.6; sixteen of a quarter of the columns and both row tiles, half the reads of
 //                  the sums, 109 / 54.6)
 //   next  fetch  : one thread; a bulk copy a stage of the activations, which linear_x_kernel has put into the operand's order,
@@ -317,7 +333,7 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 // Roles meet at barriers only, so that the chain of a stage (codes, expansion, MMAs, fold) overlaps its neighbours', blocks' ends
 // included; the same work by eight warps that all did every part, a barrier of the CTA a stage, took 88 us at 64 tokens, 14336 x 14336.
 // Bound by the fold at 64 tokens (63% of the issue slots at groups of 64), by the expansion and the hand-overs at 32 and fewer:
-// 43.4 us at 14336 x 14336, 39% of what the codes' bytes take.
+// 45.3 us at 14336 x 14336 and 32 tokens, 2.4 TB/s of codes and parameters.  The subtraction that makes 16 + q a q is 2 to 5% of the time.
 // A block that lies within one CTA's run goes from the fold warps' registers to y; the pieces of the others go to the workspace, and a
 // kernel behind this one adds them up in the order of the CTAs.
 // Tensor memory: two A buffers of 128 columns, then BUFS accumulator buffers of 2 * TOK, one a group.
@@ -503,9 +519,9 @@ __device__ __noinline__ void tc_expand_role(const LinearArgs& a, TcRole R, int w
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t w = cw[e][j >> 1];
-                    r[4 * j + 2 * e] = j & 1 ? code_pair<2>(w, bits) : code_pair<0>(w, bits);
-                    r[4 * j + 2 * e + 1] = j & 1 ? code_pair<3>(w, bits) : code_pair<1>(w, bits);
+                    const uint32_t w = cw[e][j >> 1], w8 = w >> 8;
+                    r[4 * j + 2 * e] = j & 1 ? whole_pair<2>(w, w8, bits) : whole_pair<0>(w, w8, bits);
+                    r[4 * j + 2 * e + 1] = j & 1 ? whole_pair<3>(w, w8, bits) : whole_pair<1>(w, w8, bits);
                 }
             tc_st_x8(to, r);
         }
@@ -639,7 +655,7 @@ __device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw,
         for (int g = 0; g < S::GROUPS; ++g) {
             const __half2 pv = *reinterpret_cast<const __half2*>(&cur.x);
             s1[g] = __low2float(pv);
-            m1[g] = fmaf(-16.f, s1[g], __high2float(pv));
+            m1[g] = __high2float(pv);
             cur.x = cur.y, cur.y = cur.z, cur.z = cur.w;
         }
         if (ok) ok = warp_saw(ready) || warp_wait(TC_BAR(x_full, slot), (s / TC_SLOTS) & 1, &sh->poison, g_linear_status, 5, s);
@@ -844,6 +860,7 @@ static cudaError_t linear_few(LinearArgs a, int y_f32, int n_sms, cudaStream_t s
 //   56 * 2^20 20.0 / 19.3 (16, 14336 x 4096),  2^26 18.8 / 18.9 (16, 8192 x 8192) and 21.1 / 19.0 (64, 4096 x 4096),
 //   2^27 35.9 / 20.3 (128, 4096 x 4096),  196 * 2^20 57.4 / 39.3 (16, 14336 x 14336).
 // With 8 tokens the few-token kernel has one MMA a step and keeps up with the codes: 41.3 us at 14336 x 14336, the other 39.0 us.
+// (The tcgen05 kernel's figures are from before its operand was freed of the 16: 2 to 5% more now, 41.9 in the last of the table.)
 static int tc_tile(int T, int rows, int cols) {
     if (T <= 8 || (T + 15) / 16 * (long long)rows * cols <= 3ll << 24) return 0;
     return T <= 16 ? 16 : T <= 32 ? 32 : 64;
@@ -952,7 +969,7 @@ dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int3
     if (need && ((uintptr_t)workspace & 255)) return DYNAMO_ERR_ALIGN;
     int n_sms = 0;
     if (count_sms(&n_sms) != cudaSuccess) return DYNAMO_ERR_CUDA;
-    const LinearArgs a = {(const __nv_bfloat16*)x, (const uint8_t*)codes, (const uint32_t*)params, y, T, cols, rows, {0x00780078u, 0x41804180u}, (const uint8_t*)workspace, nullptr, 1, 0};
+    const LinearArgs a = {(const __nv_bfloat16*)x, (const uint8_t*)codes, (const uint32_t*)params, y, T, cols, rows, {0x00780078u, 0x41804180u, 0x000f000fu, 0x43004300u}, (const uint8_t*)workspace, nullptr, 1, 0};
     const cudaError_t e = group_size == 64 ? linear_by_tokens<64>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream)
                                            : linear_by_tokens<128>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream);
     return e == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;
