@@ -6,9 +6,11 @@
 //   s_r = rsqrt(mean(r'^2) + eps),  n = r' s_r w_pre          (of r' in fp32, before that rounding)
 //
 // Gradient, with G the whole gradient of r' and u = w_pre dn:
-//   G  = dr' + s_r u - r' s_r^3 / d * A,            A = sum(u r')
+//   G  = dr' + s_r u - (s_r r') s_r (s_r A / d),    A = sum(u r')
 //   dr = res_scale G,  dz = block_scale g G,  dg = block_scale sum(z G) over the channel's tokens or the token's channels
-//   dy = s_y (v - y s_y^2 / d * sum(v y)),  v = dz w_post;   dw_post = sum_t dz y s_y,  dw_pre = sum_t dn r' s_r
+//   dy = s_y v - (s_y y) s_y (s_y sum(v y) / d),  v = dz w_post;   dw_post = sum_t dz y s_y,  dw_pre = sum_t dn r' s_r
+// Powers of a factor are never worked out: the cube leaves the range of fp32 at factors of 1e13 and 1e-13 (rows near zero with a tiny
+// eps, rows of large values), where the gradient does not.
 // sum(v y) is linear in A, so that A, sum(v y) with A = 0 and what multiplies A are summed in ONE reduction over the row.
 // The backward pass works r' out again from y and r, in fp32: no rounded r' enters it.
 //
@@ -362,11 +364,11 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), grad
         }
         float sum[3] = {lo(sum2[0]) + hi(sum2[0]), lo(sum2[1]) + hi(sum2[1]), lo(sum2[2]) + hi(sum2[2])};
         row_sums<TPR>(sum, scratch[turn]);
-        const float ca = s_r * s_r * s_r * inv_d * sum[0];      // G = dr' + s_r u - ca r'
-        const float zg = s_y * (sum[1] - ca * sum[2]);          // sum(k z G)
+        const float ca = s_r * (s_r * sum[0] * inv_d);             // G = dr' + s_r u - ca (s_r r')
+        const float zg = s_y * (sum[1] - ca * (s_r * sum[2]));     // sum(k z G)
         if (a.d_gate && a.gate_kind == DYNAMO_GATE_TOKEN && tt == 0) a.d_gate[t] = a.block_scale * zg;
         const float cv = a.post ? gz * zg * inv_d : 0.f;        // sum(v y) s_y / d
-        const F2 ca2 = f2(-ca), gy2 = f2(gz * s_y), cy2 = f2(-cv * s_y * s_y), sr2 = f2(s_r);
+        const F2 ca2 = f2(-ca), gy2 = f2(gz * s_y), cy2 = f2(-cv * s_y), sy2 = f2(s_y), sr2 = f2(s_r);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = 8 * (tt + i * TPR);
@@ -374,11 +376,11 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), grad
             if constexpr (!KEEP) post_weights(a, c, p[i]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const F2 G = fma2(ca2, x[i][j], g[i][j]);
+                const F2 xn = mul2(x[i][j], sr2), G = fma2(ca2, xn, g[i][j]);
                 const F2 gG = mul2(gy2, G);
                 acc[0][i][j] = fma2(gG, y[i][j], acc[0][i][j]);
-                acc[1][i][j] = fma2(dn[i][j], mul2(x[i][j], sr2), acc[1][i][j]);
-                y[i][j] = fma2(p[i][j], gG, mul2(cy2, y[i][j]));
+                acc[1][i][j] = fma2(dn[i][j], xn, acc[1][i][j]);
+                y[i][j] = fma2(p[i][j], gG, mul2(cy2, mul2(sy2, y[i][j])));
                 g[i][j] = mul2(res, G);
             }
             if (a.d_r) store8((TR*)a.d_r + t * d + c, g[i]);
@@ -496,10 +498,10 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1) norm_join_grad_wide_kernel(co
         }
         float sum[3] = {lo(sum2[0]) + hi(sum2[0]), lo(sum2[1]) + hi(sum2[1]), lo(sum2[2]) + hi(sum2[2])};
         row_sums<TPR>(sum, scratch[turn]);
-        const float ca = s_r * s_r * s_r * inv_d * sum[0], zg = s_y * (sum[1] - ca * sum[2]);
+        const float ca = s_r * (s_r * sum[0] * inv_d), zg = s_y * (sum[1] - ca * (s_r * sum[2]));
         if (a.d_gate && a.gate_kind == DYNAMO_GATE_TOKEN && tt == 0) a.d_gate[t] = a.block_scale * zg;
         const float cv = a.post ? gz * zg * inv_d : 0.f;
-        const F2 ca2 = f2(-ca), cy2 = f2(-cv * s_y * s_y);
+        const F2 ca2 = f2(-ca), cy2 = f2(-cv * s_y), sy2 = f2(s_y);
 #pragma unroll 2
         for (int i = tt; i < runs; i += TPR) {
             const int c = 8 * i;
@@ -512,11 +514,11 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1) norm_join_grad_wide_kernel(co
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const F2 G = fma2(ca2, C.x[j], C.g[j]);
+                const F2 xn = mul2(C.x[j], sr2), G = fma2(ca2, xn, C.g[j]);
                 const F2 gG = mul2(gy2, G);
                 s1[j] = fma2(gG, C.y[j], s1[j]);
-                s2[j] = fma2(C.dn[j], mul2(C.x[j], sr2), s2[j]);
-                C.y[j] = fma2(C.p[j], gG, mul2(cy2, C.y[j]));
+                s2[j] = fma2(C.dn[j], xn, s2[j]);
+                C.y[j] = fma2(C.p[j], gG, mul2(cy2, mul2(sy2, C.y[j])));
                 C.g[j] = mul2(res, G);
             }
             if (a.part) {
