@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(DISPATCH_THREADS, 1) dispatch_kernel(const __g
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int k = a.k, E = a.E;
     const long long n_pairs = (long long)a.T * k;
-    const int t0 = blockIdx.x * a.seg, t1 = min(a.T, t0 + a.seg);
+    const int t0 = blockIdx.x * a.seg, t1 = t0 + min(a.seg, a.T - t0);   // (T may be 2^31 - 1)
     const long long lo = (long long)t0 * k;
     if (tid < DISPATCH_EXPERTS) {
         s_total[tid] = 0;
@@ -125,8 +125,8 @@ __global__ void __launch_bounds__(DISPATCH_THREADS, 1) dispatch_kernel(const __g
     }
     const unsigned lt = (1u << lane) - 1;
     const int chunk_tokens = DISPATCH_CHUNK / k;
-    for (int c0 = t0; c0 < t1; c0 += chunk_tokens) {
-        const int c1 = min(t1, c0 + chunk_tokens);
+    for (int c0 = t0, c1; c0 < t1; c0 = c1) {
+        c1 = c0 + min(chunk_tokens, t1 - c0);
         const int n = (c1 - c0) * k;
         const long long base = (long long)c0 * k;
         const int piece = ((n + 31) / 32 + DISPATCH_WARPS - 1) / DISPATCH_WARPS * 32;   // whole batches of 32 a warp
