@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(256) combine_grad_kernel(const TY* __restrict_
             at[j] = place_of(pos[(long long)t * K + j], T * K);
             wt[j] = w ? w[(long long)t * K + j] : 1.f;
         }
-        for (int c = tt * 8; c < d; c += tpt * 8) {
+        for (uint32_t c = tt * 8; c < (uint32_t)d; c += tpt * 8) {   // (a step past the last of nearly 2^31 columns)
             const Raw8<TY> g = load8(dy + (long long)t * d + c);
             Raw8<TR> raw[K];
 #pragma unroll

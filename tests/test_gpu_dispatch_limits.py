@@ -26,3 +26,17 @@ def test_pairs_up_to_two_to_the_31(T):
         at = first[t % E] + t // E
         assert torch.equal(pos[i:i + step, 0].long(), at)
         assert torch.equal(perm[at].long(), t)
+
+
+def test_rows_of_two_to_the_31_values():
+    """One token: every run of eight columns up to the last is in the sum and in the gradients, and nothing else is touched."""
+    d = 2 ** 31 - 8
+    rows = torch.zeros((1, d), dtype=torch.bfloat16, device="cuda")
+    rows[0, :8], rows[0, -8:] = 1.0, 2.0
+    w = torch.tensor([[0.5]], device="cuda")
+    s = ops.dispatch(torch.zeros((1, 1), dtype=torch.int32, device="cuda"), 1, rows)
+    assert torch.equal(s.rows, rows)
+    y = ops.combine(s.rows, s.pos, w)
+    assert (y[0, :8] == 0.5).all() and (y[0, -8:] == 1.0).all() and int(torch.count_nonzero(y)) == 16
+    d_rows, d_w = ops.combine_backward(rows, s.rows, s.pos, w)
+    assert torch.equal(d_rows, y) and d_w.item() == 8 * 1.0 + 8 * 4.0
