@@ -735,7 +735,9 @@ dynamo_status dynamo_norm_join_backward(const dynamo_join_desc* desc, const void
             if constexpr (L::V == 0) {
                 auto wide = [&](auto kernel) {
                     const size_t sums = a.part ? 2 * (size_t)desc->d * sizeof(float) : 0;
-                    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sums);
+                    // (the widest row's, whatever this one's: the limit is the function's, and other threads launch it too)
+                    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                               2 * JOIN_MAX_D * (int)sizeof(float));
                     return e != cudaSuccess ? e : launch_pdl(kernel, grid, block, sums, st, a);
                 };
                 return a.n_f32 ? wide(norm_join_grad_wide_kernel<TY, TR, float>) : wide(norm_join_grad_wide_kernel<TY, TR, __nv_bfloat16>);
