@@ -609,10 +609,13 @@ __global__ void __launch_bounds__(FFN_THREADS, (MAXNT8 <= 2 && APW == 2) ? 3 : 2
     if (fills && (!EITHER || blockIdx.x == 0)) pdl_wait();
 }
 
+constexpr int SMEM_THREE = 74 * 1024, SMEM_TWO = 110 * 1024;   // of a CTA, with three and with two an SM
+
 template <bool GATEUP, int MAXNT8, int G>
 static cudaError_t launch_one_g(const FfnParams& p, int n_ctas, cudaStream_t st) {
     auto kernel = p.few ? ffn_stream_kernel<GATEUP, MAXNT8, G, true> : ffn_stream_kernel<GATEUP, MAXNT8, G, false>;
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem_bytes);
+    // (the limit is the function's, and other threads launch it for other layers: always the larger ring's)
+    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_TWO);
     if (err != cudaSuccess) return err;
     return launch_pdl(kernel, dim3((unsigned)n_ctas), dim3(FFN_THREADS), (size_t)p.smem_bytes, st, p);
 }
@@ -634,7 +637,7 @@ cudaError_t launch_ffn_stream(const LayerDev* L, const WsDev& ws, int gateup, in
                               long long split_stride, int tiles, long long n_items, bool long_rows, int few, bool fills,
                               bool leads, int n_sms, int G, cudaStream_t st) {
     const bool three = tiles < 3 && APW == 2 && n_items > 3 * n_sms;
-    const int smem_bytes = three ? 74 * 1024 : 110 * 1024;
+    const int smem_bytes = three ? SMEM_THREE : SMEM_TWO;
     const int n_ctas = (three ? 3 : 2) * n_sms;
     FfnParams p;
     p.L = L;

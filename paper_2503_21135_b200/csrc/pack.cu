@@ -215,7 +215,8 @@ cudaError_t launch_pack_blocks(const void* src_a, const void* src_b, int n_rows_
                                int fused, void* dst, cudaStream_t st) {
     const int blk = block_bytes(bits, G);
     dim3 grid(K / KC, n_rows_blocks);
-    cudaError_t err = cudaFuncSetAttribute(pack_blocks_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, blk);
+    // (the largest block's, whatever this one's: the limit is the function's, and other threads launch it too)
+    cudaError_t err = cudaFuncSetAttribute(pack_blocks_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, block_bytes(HI_BITS, 64));
     if (err != cudaSuccess) return err;
     pack_blocks_kernel<<<grid, 256, blk, st>>>((const __nv_bfloat16*)src_a, (const __nv_bfloat16*)src_b, K, G, bits,
                                                fused, (uint8_t*)dst, blk, K / KC);
