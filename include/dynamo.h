@@ -203,7 +203,7 @@ dynamo_status dynamo_expert_stream_bytes(dynamo_ctx* ctx, int32_t expert, size_t
  * activation was clamped (see Conventions); outputs are defined.  TIMEOUT wins when both are set.  Else DYNAMO_OK. */
 dynamo_status dynamo_poll_status(dynamo_ctx* ctx, void* stream);
 
-/* Debug calls.  (The paper has no counterpart.)
+/* Debug calls.  (The paper has no counterpart.  dynamo_debug_expire_linear stands with the call that it exercises.)
  * dynamo_debug_expire_wait: launches one warp that waits, through the same bounded wait the FFN kernels use but with
  *   limit_ns (1e3 .. 1e8) as its limit, on a barrier that nobody arrives at.  The wait gives up, sets the TIMEOUT
  *   status bit and the kernel returns: nothing faults or hangs.  Exercises the failure path end to end
@@ -481,6 +481,13 @@ dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int3
                                     void* workspace, size_t workspace_bytes, void* stream);
 dynamo_status dynamo_linear_workspace_bytes(int32_t T, int32_t rows, int32_t cols, int32_t group_size, size_t* bytes);
 dynamo_status dynamo_linear_poll_status(void* stream);
+
+/* Debug call: dynamo_linear_forward, but the activations of one step are never brought, so that the bounded waits of one part of the
+ * launch run out (after about a second; that part of y, always the first element, is NaN, the rest as ever) and the status is set;
+ * nothing faults or hangs.  Calls without such waits (those that need no workspace) are refused (ERR_ARG). */
+dynamo_status dynamo_debug_expire_linear(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size,
+                                         const void* codes, const void* params, void* y, int32_t y_dtype,
+                                         void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -43,7 +43,7 @@ EXPORTED = ["dynamo_create", "dynamo_destroy", "dynamo_arena_bytes", "dynamo_pac
             "dynamo_norm_join_forward", "dynamo_norm_join_workspace_bytes", "dynamo_norm_join_backward",
             "dynamo_moe_block_forward",
             "dynamo_linear_quantize", "dynamo_linear_forward", "dynamo_linear_workspace_bytes",
-            "dynamo_linear_poll_status",
+            "dynamo_linear_poll_status", "dynamo_debug_expire_linear",
             "dynamo_kernel_launches", "dynamo_status_str"]
 
 
@@ -122,6 +122,7 @@ def load():
         L.dynamo_moe_block_forward.argtypes = [vp, jd, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
         L.dynamo_linear_quantize.argtypes = [vp, i32, i32, i32, vp, vp, vp]
         L.dynamo_linear_forward.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp, sz, vp]
+        L.dynamo_debug_expire_linear.argtypes = L.dynamo_linear_forward.argtypes
         L.dynamo_linear_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.dynamo_linear_poll_status.argtypes = [vp]
         L.dynamo_kernel_launches.argtypes = [vp]

@@ -94,6 +94,7 @@ struct LinearArgs {
     const uint8_t* xt;        // tcgen05 kernel: activations in its order
     float* part;              // and partial results, two tiles a CTA
     int n_split, units;       // shares of the input indices (CTAs of a cluster), units of LIN_UNIT in a share
+    int withhold;             // 1 (dynamo_debug_expire_linear): the first CTA's first stage of activations is never brought
 };
 
 constexpr int LIN_WARPS = 8;
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 //                  row's codes; a row a lane kept the L1 busy with 32 lines a load).  The codes come by cp.async, three jobs of a warp
 //                  on their way: 96 KB an SM (one job in registers left the loads' latency to bind)
 //   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + m * sum(x); sixteen warps at 64
-//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 81.4 / 56.6 us; as 78.3 / 55.4 they were compared, before the
+//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 81.4 / 57.5 us; as 78.3 / 55.4 they were compared, before the
 //                  operand's 16 went off in the expansion, with packed pairs, whose moves and registers cost more than the instructions
 //                  they save, 85.1 / 54.1, and both halves of the columns on their way
 //                  90.0 / 53.7, spilling; eight warps 107 / 50.6; sixteen of a quarter of the columns and both row tiles, half the reads of
@@ -333,11 +334,13 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 // Roles meet at barriers only, so that the chain of a stage (codes, expansion, MMAs, fold) overlaps its neighbours', blocks' ends
 // included; the same work by eight warps that all did every part, a barrier of the CTA a stage, took 88 us at 64 tokens, 14336 x 14336.
 // Bound by the fold at 64 tokens (63% of the issue slots at groups of 64), by the expansion and the hand-overs at 32 and fewer:
-// 45.3 us at 14336 x 14336 and 32 tokens, 2.4 TB/s of codes and parameters.  The subtraction that makes 16 + q a q is 2 to 5% of the time.
+// 45.8 us at 14336 x 14336 and 32 tokens, 2.4 TB/s of codes and parameters.  The subtraction that makes 16 + q a q is 2 to 5% of the time.
 // A block that lies within one CTA's run goes from the fold warps' registers to y; the pieces of the others go to the workspace, and a
 // kernel behind this one adds them up in the order of the CTAs.
 // Tensor memory: two A buffers of 128 columns, then BUFS accumulator buffers of 2 * TOK, one a group.
-// Every wait is bounded; after an expired one the roles end, the CTA's remaining results are NaN and the status word is set.
+// Every wait is bounded; after an expired one the roles end (and arrive at no barrier any more: a stage that was not waited for is not
+// handed on), the CTA's remaining results are NaN and the status word is set.  Copies and MMAs that are still under way then have
+// a while to end before the CTA's shared and tensor memory goes away.
 constexpr int TC_ROWS = 256;
 constexpr int TC_SLOTS = 4;       // stages of activations on their way or in use
 constexpr int TC_JOBS = 3;        // jobs (four atoms of a stage) of an expand warp whose codes are on their way or in use
@@ -673,7 +676,7 @@ __device__ __noinline__ void tc_fold_role(const LinearArgs& a, TcRole R, int fw,
             }
         }
         __syncwarp();
-        if (lane == 0) bar_arrive(TC_BAR(x_empty, slot));
+        if (ok && lane == 0) bar_arrive(TC_BAR(x_empty, slot));
 #pragma unroll
         for (int g = 0; g < S::GROUPS; ++g) {
             if (g >= ng) break;
@@ -777,13 +780,9 @@ __global__ void __launch_bounds__(32 * TcShape<TOK, G>::WARPS, 1) linear_tc_kern
                 if (s >= TC_SLOTS)
                     ok = mbar_wait_bounded(&sh.x_empty[slot], ((s / TC_SLOTS) & 1) ^ 1, &sh.poison, g_linear_status, WAIT_LIMIT_NS, 7, s);
                 if (!ok) break;
+                if (a.withhold && blockIdx.x == 0 && s == 0) continue;
                 mbar_arrive_expect_tx(&sh.x_full[slot], S::XB);
                 bulk_g2s(smem + S::CODES + slot * S::XB, a.xt + ((long long)pos.tile * R.stages + pos.u) * S::XB, S::XB, &sh.x_full[slot]);
-            }
-            if (!ok) {   // let copies in flight land before the CTA's shared memory goes away
-                const unsigned long long t = globaltimer_ns();
-                while (globaltimer_ns() - t < 2000000ull) {
-                }
             }
         }
         __syncwarp();
@@ -793,6 +792,13 @@ __global__ void __launch_bounds__(32 * TcShape<TOK, G>::WARPS, 1) linear_tc_kern
     }
     tc_fence_before();
     __syncthreads();
+    if (sh.poison) {
+        // what the roles that gave up had begun: bulk copies into the ring, MMAs that read it and write tensor memory
+        const unsigned long long t = globaltimer_ns();
+        while (globaltimer_ns() - t < 2000000ull) {
+        }
+        __syncthreads();
+    }
     if (warp == S::W_MMA) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(R.tm), "n"(TC_COLS) : "memory");
@@ -860,7 +866,7 @@ static cudaError_t linear_few(LinearArgs a, int y_f32, int n_sms, cudaStream_t s
 //   56 * 2^20 20.0 / 19.3 (16, 14336 x 4096),  2^26 18.8 / 18.9 (16, 8192 x 8192) and 21.1 / 19.0 (64, 4096 x 4096),
 //   2^27 35.9 / 20.3 (128, 4096 x 4096),  196 * 2^20 57.4 / 39.3 (16, 14336 x 14336).
 // With 8 tokens the few-token kernel has one MMA a step and keeps up with the codes: 41.3 us at 14336 x 14336, the other 39.0 us.
-// (The tcgen05 kernel's figures are from before its operand was freed of the 16: 2 to 5% more now, 41.9 in the last of the table.)
+// (The tcgen05 kernel's figures are from before its operand was freed of the 16: 2 to 5% more now, 42.2 in the last of the table.)
 static int tc_tile(int T, int rows, int cols) {
     if (T <= 8 || (T + 15) / 16 * (long long)rows * cols <= 3ll << 24) return 0;
     return T <= 16 ? 16 : T <= 32 ? 32 : 64;
@@ -917,6 +923,29 @@ dynamo_status check_linear(int32_t rows, int32_t cols, int32_t group_size) {
     return DYNAMO_OK;
 }
 
+dynamo_status linear_impl(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size, const void* codes, const void* params,
+                          void* y, int32_t y_dtype, void* workspace, size_t workspace_bytes, int withhold, void* stream) {
+    if (const dynamo_status s = check_linear(rows, cols, group_size); s != DYNAMO_OK) return s;
+    if (y_dtype != DYNAMO_BF16 && y_dtype != DYNAMO_F32) return DYNAMO_ERR_SHAPE;
+    if (T < 0 || T > DYNAMO_LINEAR_MAX_TOKENS) return DYNAMO_ERR_TOKENS;
+    if (T == 0) return DYNAMO_OK;
+    if (!x || !codes || !params || !y) return DYNAMO_ERR_NULL;
+    if (!aligned16(x, codes, params, y)) return DYNAMO_ERR_ALIGN;
+    // (the tcgen05 kernel counts its stages, a tile of tokens by 256 rows by 128 columns each, in 32 bits)
+    if ((long long)(T / 16 + 1) * (rows / 256 + 1) * (cols / 128 + 1) > 0x7fffffffll) return DYNAMO_ERR_TOKENS;
+    const size_t need = tc_workspace(T, rows, cols, group_size);
+    if (need && !workspace) return DYNAMO_ERR_NULL;
+    if (workspace_bytes < need) return DYNAMO_ERR_ARENA_TOO_SMALL;
+    if (need && ((uintptr_t)workspace & 255)) return DYNAMO_ERR_ALIGN;
+    int n_sms = 0;
+    if (count_sms(&n_sms) != cudaSuccess) return DYNAMO_ERR_CUDA;
+    const LinearArgs a = {(const __nv_bfloat16*)x, (const uint8_t*)codes, (const uint32_t*)params, y, T, cols, rows,
+                          {0x00780078u, 0x41804180u, 0x000f000fu, 0x43004300u}, (const uint8_t*)workspace, nullptr, 1, 0, withhold};
+    const cudaError_t e = group_size == 64 ? linear_by_tokens<64>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream)
+                                           : linear_by_tokens<128>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream);
+    return e == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -955,24 +984,16 @@ dynamo_status dynamo_linear_poll_status(void* stream) {
 dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size, const void* codes,
                                     const void* params, void* y, int32_t y_dtype, void* workspace, size_t workspace_bytes,
                                     void* stream) {
+    return linear_impl(x, T, rows, cols, group_size, codes, params, y, y_dtype, workspace, workspace_bytes, 0, stream);
+}
+
+dynamo_status dynamo_debug_expire_linear(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size, const void* codes,
+                                         const void* params, void* y, int32_t y_dtype, void* workspace, size_t workspace_bytes,
+                                         void* stream) {
     if (const dynamo_status s = check_linear(rows, cols, group_size); s != DYNAMO_OK) return s;
-    if (y_dtype != DYNAMO_BF16 && y_dtype != DYNAMO_F32) return DYNAMO_ERR_SHAPE;
     if (T < 0 || T > DYNAMO_LINEAR_MAX_TOKENS) return DYNAMO_ERR_TOKENS;
-    if (T == 0) return DYNAMO_OK;
-    if (!x || !codes || !params || !y) return DYNAMO_ERR_NULL;
-    if (!aligned16(x, codes, params, y)) return DYNAMO_ERR_ALIGN;
-    // (the tcgen05 kernel counts its stages, a tile of tokens by 256 rows by 128 columns each, in 32 bits)
-    if ((long long)(T / 16 + 1) * (rows / 256 + 1) * (cols / 128 + 1) > 0x7fffffffll) return DYNAMO_ERR_TOKENS;
-    const size_t need = tc_workspace(T, rows, cols, group_size);
-    if (need && !workspace) return DYNAMO_ERR_NULL;
-    if (workspace_bytes < need) return DYNAMO_ERR_ARENA_TOO_SMALL;
-    if (need && ((uintptr_t)workspace & 255)) return DYNAMO_ERR_ALIGN;
-    int n_sms = 0;
-    if (count_sms(&n_sms) != cudaSuccess) return DYNAMO_ERR_CUDA;
-    const LinearArgs a = {(const __nv_bfloat16*)x, (const uint8_t*)codes, (const uint32_t*)params, y, T, cols, rows, {0x00780078u, 0x41804180u, 0x000f000fu, 0x43004300u}, (const uint8_t*)workspace, nullptr, 1, 0};
-    const cudaError_t e = group_size == 64 ? linear_by_tokens<64>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream)
-                                           : linear_by_tokens<128>(a, y_dtype == DYNAMO_F32, n_sms, (cudaStream_t)stream);
-    return e == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;
+    if (!tc_tile(T, rows, cols)) return DYNAMO_ERR_ARG;   // the few-token kernel waits for nothing
+    return linear_impl(x, T, rows, cols, group_size, codes, params, y, y_dtype, workspace, workspace_bytes, 1, stream);
 }
 
 }  // extern "C"
