@@ -385,7 +385,8 @@ dynamo_status dynamo_route_permute_static(const float* router_logits, int32_t T,
 /* ---- Operators around the layer --------------------------------------------------------------------------------------
  * What a decoder block needs next to dynamo_moe_forward.  They take no context (but dynamo_moe_block_forward does):
  * device buffers, sizes and a stream, which has to belong to the current device.  Every call is asynchronous and stream-
- * ordered, can be captured in a CUDA graph, keeps nothing between calls and gives the same bits for the same inputs (no
+ * ordered, can be captured in a CUDA graph, keeps nothing between calls (of dynamo_linear_forward a status stays on the device where a
+ * bounded wait has expired, see dynamo_linear_poll_status) and gives the same bits for the same inputs (no
  * floating-point atomics).  Row-major contiguous arrays, 16-byte aligned (ERR_ALIGN); a *_dtype is DYNAMO_BF16 or
  * DYNAMO_F32 (ERR_SHAPE otherwise); widths are multiples of 8 (ERR_SHAPE).  Outputs must not overlap inputs or one
  * another unless stated.  Sums, norms and weights are worked out in fp32, results rounded once.  T = 0 is a no-op unless
@@ -469,8 +470,10 @@ dynamo_status dynamo_moe_block_forward(dynamo_ctx* ctx, const dynamo_join_desc* 
  *   once per 64 tokens, small ones (16 tokens x the matrix up to 3 * 2^24) per 16.  A NaN activation makes its token's row NaN, an
  *   infinite one makes it infinite or NaN; the sum of 31 |x| over a group has to stay in the range of fp32.
  *   workspace: dynamo_linear_workspace_bytes (0 for up to 8 tokens and small matrices: then it may be NULL), 256-byte aligned.
- * dynamo_linear_poll_status: synchronises the stream; DYNAMO_ERR_TIMEOUT if a bounded wait of dynamo_linear_forward expired on the
- *   current device since the last call (the results concerned are NaN), else DYNAMO_OK.
+ * dynamo_linear_poll_status: synchronises the stream; DYNAMO_ERR_TIMEOUT if a bounded wait of dynamo_linear_forward has expired on the
+ *   current device (the results concerned are NaN), else DYNAMO_OK.  All calls on a device share the status and the answer stays the
+ *   same, so that every user of it is told.  dynamo_linear_clear_status synchronises the stream and sets it back: for the
+ *   program that knows them all.
  * group_size 64 or 128, cols a multiple of it, both up to 2^24, rows >= 1 (ERR_SHAPE); 0 <= T <= DYNAMO_LINEAR_MAX_TOKENS, and
  *   T * rows * cols below 2^50 or so (ERR_TOKENS). */
 #define DYNAMO_LINEAR_MAX_TOKENS 65536
@@ -481,6 +484,7 @@ dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int3
                                     void* workspace, size_t workspace_bytes, void* stream);
 dynamo_status dynamo_linear_workspace_bytes(int32_t T, int32_t rows, int32_t cols, int32_t group_size, size_t* bytes);
 dynamo_status dynamo_linear_poll_status(void* stream);
+dynamo_status dynamo_linear_clear_status(void* stream);
 
 /* Debug call: dynamo_linear_forward, but the activations of one step are never brought, so that the bounded waits of one part of the
  * launch run out (after about a second; that part of y, always the first element, is NaN, the rest as ever) and the status is set;

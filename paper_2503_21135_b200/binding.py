@@ -43,7 +43,7 @@ EXPORTED = ["dynamo_create", "dynamo_destroy", "dynamo_arena_bytes", "dynamo_pac
             "dynamo_norm_join_forward", "dynamo_norm_join_workspace_bytes", "dynamo_norm_join_backward",
             "dynamo_moe_block_forward",
             "dynamo_linear_quantize", "dynamo_linear_forward", "dynamo_linear_workspace_bytes",
-            "dynamo_linear_poll_status", "dynamo_debug_expire_linear",
+            "dynamo_linear_poll_status", "dynamo_linear_clear_status", "dynamo_debug_expire_linear",
             "dynamo_kernel_launches", "dynamo_status_str"]
 
 
@@ -125,6 +125,7 @@ def load():
         L.dynamo_debug_expire_linear.argtypes = L.dynamo_linear_forward.argtypes
         L.dynamo_linear_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.dynamo_linear_poll_status.argtypes = [vp]
+        L.dynamo_linear_clear_status.argtypes = [vp]
         L.dynamo_kernel_launches.argtypes = [vp]
         L.dynamo_kernel_launches.restype = ctypes.c_int64
         L.dynamo_status_str.argtypes = [i32]

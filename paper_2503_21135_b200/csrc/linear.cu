@@ -975,10 +975,13 @@ dynamo_status dynamo_linear_poll_status(void* stream) {
     if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return DYNAMO_ERR_CUDA;
     int32_t word = 0;
     if (cudaMemcpyFromSymbol(&word, g_linear_status, 4) != cudaSuccess) return DYNAMO_ERR_CUDA;
-    if (word == 0) return DYNAMO_OK;
+    return word == 0 ? DYNAMO_OK : DYNAMO_ERR_TIMEOUT;   // (and it stays: other users of the device ask too)
+}
+
+dynamo_status dynamo_linear_clear_status(void* stream) {
+    if (cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return DYNAMO_ERR_CUDA;
     const int32_t zero[16] = {};
-    if (cudaMemcpyToSymbol(g_linear_status, zero, sizeof(zero)) != cudaSuccess) return DYNAMO_ERR_CUDA;
-    return DYNAMO_ERR_TIMEOUT;
+    return cudaMemcpyToSymbol(g_linear_status, zero, sizeof(zero)) == cudaSuccess ? DYNAMO_OK : DYNAMO_ERR_CUDA;
 }
 
 dynamo_status dynamo_linear_forward(const void* x, int32_t T, int32_t rows, int32_t cols, int32_t group_size, const void* codes,

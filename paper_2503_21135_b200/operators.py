@@ -17,7 +17,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from .binding import BF16, F32, DynamoError, load
+from .binding import BF16, F32, OK, DynamoError, load
 
 _native = None
 
@@ -109,5 +109,12 @@ def linear(x: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, y_dtype: 
 
 def poll_linear_status() -> int:
     """Waits for the current stream.  0, or the library's ERR_TIMEOUT if a bounded wait of ``linear`` has expired on the current
-    device since the last call: results of that time that are NaN are lost."""
+    device: results that are NaN are lost.  Every caller is told, until ``clear_linear_status``."""
     return load().dynamo_linear_poll_status(torch.cuda.current_stream().cuda_stream)
+
+
+def clear_linear_status() -> None:
+    """Waits for the current stream and sets the status of ``poll_linear_status`` back to 0, for all users of the device."""
+    st = load().dynamo_linear_clear_status(torch.cuda.current_stream().cuda_stream)
+    if st != OK:
+        raise DynamoError(st, "dynamo_linear_clear_status")

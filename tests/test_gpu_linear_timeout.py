@@ -1,6 +1,7 @@
 """A bounded wait of the 4-bit product that runs out: the results concerned are NaN, the others are right, the status says so, and the
 GPU goes on as before."""
 import ctypes
+import threading
 
 import pytest
 import torch
@@ -10,6 +11,12 @@ from paper_2503_21135_b200 import operators as ops
 
 pytestmark = pytest.mark.gpu
 TIMEOUT = binding.STATUS_NAMES.index("ERR_TIMEOUT")
+
+
+@pytest.fixture(autouse=True)
+def status_set_back():
+    yield
+    ops.clear_linear_status()
 
 
 def expired(x, codes, params, G):
@@ -40,3 +47,19 @@ def test_results_behind_an_expired_wait(T, N, K, G, lost):
     assert nan[0, 0] and nan[:lost[0], :lost[1]].all() and int(nan.sum()) == lost[0] * lost[1]
     assert torch.equal(y[~nan], want[~nan])
     assert torch.equal(ops.linear(x, codes, params), want)
+
+
+def test_every_user_is_told():
+    """One user's question does not take the answer from another, in this thread or the next."""
+    codes, params = ops.quantize_linear(torch.ones((4352, 4096), dtype=torch.bfloat16, device="cuda"), 128)
+    x = torch.ones((40, 4096), dtype=torch.bfloat16, device="cuda")
+    expired(x, codes, params, 128)
+    answers = [ops.poll_linear_status(), ops.poll_linear_status(), binding.load().dynamo_linear_poll_status(None)]
+    other = threading.Thread(target=lambda: answers.append(ops.poll_linear_status()))
+    other.start()
+    other.join()
+    ops.linear(x, codes, params)          # a call that goes well changes nothing
+    answers.append(ops.poll_linear_status())
+    assert answers == [TIMEOUT] * 5
+    ops.clear_linear_status()
+    assert ops.poll_linear_status() == 0
