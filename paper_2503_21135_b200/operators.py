@@ -17,9 +17,10 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from .binding import BF16, F32, OK, DynamoError, load
+from .binding import BF16, F32, OK, STATUS_NAMES, DynamoError, load
 
 _native = None
+_ERR_TIMEOUT = STATUS_NAMES.index("ERR_TIMEOUT")
 
 
 def _lib():
@@ -107,14 +108,20 @@ def linear(x: torch.Tensor, codes: torch.Tensor, params: torch.Tensor, y_dtype: 
     return _lib().linear(x, codes, params, y_dtype, out)
 
 
-def poll_linear_status() -> int:
-    """Waits for the current stream.  0, or the library's ERR_TIMEOUT if a bounded wait of ``linear`` has expired on the current
-    device: results that are NaN are lost.  Every caller is told, until ``clear_linear_status``."""
-    return load().dynamo_linear_poll_status(torch.cuda.current_stream().cuda_stream)
+def poll_linear_status(device=None) -> int:
+    """Waits for the device's (the current one's) current stream.  0, or the library's ERR_TIMEOUT if a bounded wait of ``linear`` has
+    expired on it: results that are NaN are lost.  Every caller is told, until ``clear_linear_status``.  Raises DynamoError if the
+    status cannot be read."""
+    with torch.cuda.device(device):
+        st = load().dynamo_linear_poll_status(torch.cuda.current_stream().cuda_stream)
+    if st not in (OK, _ERR_TIMEOUT):
+        raise DynamoError(st, "dynamo_linear_poll_status")
+    return st
 
 
-def clear_linear_status() -> None:
-    """Waits for the current stream and sets the status of ``poll_linear_status`` back to 0, for all users of the device."""
-    st = load().dynamo_linear_clear_status(torch.cuda.current_stream().cuda_stream)
+def clear_linear_status(device=None) -> None:
+    """Waits for the device's current stream and sets the status of ``poll_linear_status`` back to 0, for all users of the device."""
+    with torch.cuda.device(device):
+        st = load().dynamo_linear_clear_status(torch.cuda.current_stream().cuda_stream)
     if st != OK:
         raise DynamoError(st, "dynamo_linear_clear_status")
