@@ -140,10 +140,20 @@ def status_str(status: int) -> str:
     return load().dynamo_status_str(int(status)).decode()
 
 
+class BadArgument(ValueError, AssertionError):
+    """A tensor or array of another type, size or place than a call takes.  (AssertionError as well: callers may catch it as that.)"""
+
+
+def _want(ok: bool, what: str) -> None:
+    # (not an assert statement: without these checks, under ``python -O``, wrong sizes would reach the kernels)
+    if not ok:
+        raise BadArgument(what)
+
+
 def _i32p(a: Optional[np.ndarray]):
     if a is None:
         return ctypes.cast(None, ctypes.POINTER(ctypes.c_int32))
-    assert a.dtype == np.int32 and a.flags["C_CONTIGUOUS"]
+    _want(a.dtype == np.int32 and a.flags["C_CONTIGUOUS"], "a contiguous int32 array is wanted")
     return a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
 
@@ -287,7 +297,7 @@ class DynamoLayer:
         if self.workspace is None or self.workspace.numel() < sb:
             self.workspace = torch.empty(sb, dtype=torch.uint8, device=self.device)
         for w in (w_gate, w_up, w_down):
-            assert w.is_cuda and w.dtype == torch.bfloat16 and w.is_contiguous()
+            _want(w.is_cuda and w.dtype == torch.bfloat16 and w.is_contiguous(), "w_gate, w_up, w_down: contiguous bfloat16 CUDA tensors are wanted")
         st = dynamo_pack_experts(self.ctx, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), bits, cache_idx,
                                  self.arena.data_ptr(), self.arena.numel(), self.workspace.data_ptr(),
                                  self.workspace.numel(), _stream())
@@ -312,8 +322,8 @@ class DynamoLayer:
         """Channel cache on the d_ff side: cache_idx_down int [E, P2] (sorted hidden-unit indices per expert)."""
         bits = np.ascontiguousarray(bits, dtype=np.int32)
         ci = np.ascontiguousarray(cache_idx_down, dtype=np.int32)
-        assert ci.ndim == 2 and ci.shape[0] == self.desc.n_experts
-        assert w_down.is_cuda and w_down.dtype == torch.bfloat16 and w_down.is_contiguous()
+        _want(ci.ndim == 2 and ci.shape[0] == self.desc.n_experts, "cache_idx_down: [E, P2] is wanted")
+        _want(w_down.is_cuda and w_down.dtype == torch.bfloat16 and w_down.is_contiguous(), "w_down: a contiguous bfloat16 CUDA tensor is wanted")
         P2 = int(ci.shape[1])
         nbytes = ctypes.c_size_t(0)
         _check(load().dynamo_down_cache_bytes(ctypes.byref(self.desc), _i32p(bits), P2, int(max_sig_down),
@@ -342,8 +352,8 @@ class DynamoLayer:
 
     def forward(self, x: torch.Tensor, logits: torch.Tensor, y_dtype=F32, debug=False, y: Optional[torch.Tensor] = None):
         T = x.shape[0]
-        assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous()
-        assert logits.is_cuda and logits.dtype == torch.float32 and logits.is_contiguous()
+        _want(x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous(), "x: a contiguous bfloat16 CUDA tensor is wanted")
+        _want(logits.is_cuda and logits.dtype == torch.float32 and logits.is_contiguous(), "logits: a contiguous float32 CUDA tensor is wanted")
         if y is None:
             y = torch.empty((T, self.desc.d_model), dtype=torch.float32 if y_dtype == F32 else torch.bfloat16,
                             device=x.device)
@@ -365,10 +375,10 @@ class DynamoLayer:
         """Forward with the router GEMM + top-k fused in front; returns y (, logits) (, debug outputs)."""
         T = x.shape[0]
         E, k = self.desc.n_experts, self.desc.top_k
-        assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous()
-        assert w_router.is_cuda and w_router.dtype == torch.bfloat16 and w_router.is_contiguous()
-        assert tuple(w_router.shape) == (E, self.desc.d_model)
-        assert bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.numel() == E)
+        _want(x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous(), "x: a contiguous bfloat16 CUDA tensor is wanted")
+        _want(w_router.is_cuda and w_router.dtype == torch.bfloat16 and w_router.is_contiguous(), "w_router: a contiguous bfloat16 CUDA tensor is wanted")
+        _want(tuple(w_router.shape) == (E, self.desc.d_model), "w_router: [E, d] is wanted")
+        _want(bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.numel() == E), "bias: a float32 CUDA tensor [E] is wanted")
         y = torch.empty((T, self.desc.d_model), dtype=torch.float32 if y_dtype == F32 else torch.bfloat16, device=x.device)
         lg = torch.empty((T, E), dtype=torch.float32, device=x.device) if want_logits else None
         dbg, outs = None, None
@@ -402,16 +412,16 @@ class DynamoLayer:
             rows.append(gate)
         given = [r, n, w_router] + [t for t in (bias, w_post, gate, w_pre, y) if t is not None]
         device = r.device if self.workspace is None else self.workspace.device   # (no weights yet: the call itself refuses)
-        assert all(t.is_cuda and t.is_contiguous() and t.device == device for t in given)
-        assert d == self.desc.d_model and r.dtype in types and n.shape == r.shape and n.dtype == torch.bfloat16
-        assert tuple(w_router.shape) == (self.desc.n_experts, d) and w_router.dtype == torch.bfloat16
-        assert bias is None or (bias.dtype == torch.float32 and bias.numel() == self.desc.n_experts)
-        assert all(w.shape == (d,) and w.dtype in types and w.dtype == rows[0].dtype for w in rows)
-        assert not per_token or (tuple(gate.shape) == (T, 1) and gate.dtype == torch.float32)
-        assert (post_norm or w_post is None) and (pre_norm or w_pre is None)
+        _want(all(t.is_cuda and t.is_contiguous() and t.device == device for t in given), "contiguous tensors on the layer's CUDA device are wanted")
+        _want(d == self.desc.d_model and r.dtype in types and n.shape == r.shape and n.dtype == torch.bfloat16, "r: [T, d] bfloat16 or float32, and n: [T, d] bfloat16 are wanted")
+        _want(tuple(w_router.shape) == (self.desc.n_experts, d) and w_router.dtype == torch.bfloat16, "w_router: bfloat16 [E, d] is wanted")
+        _want(bias is None or (bias.dtype == torch.float32 and bias.numel() == self.desc.n_experts), "bias: float32 [E] is wanted")
+        _want(all(w.shape == (d,) and w.dtype in types and w.dtype == rows[0].dtype for w in rows), "w_post, w_pre and a gate of the channels: [d], bfloat16 or float32, one type for all is wanted")
+        _want(not per_token or (tuple(gate.shape) == (T, 1) and gate.dtype == torch.float32), "gate: [d] or float32 [T, 1] is wanted")
+        _want((post_norm or w_post is None) and (pre_norm or w_pre is None), "w_post goes with post_norm, w_pre with pre_norm")
         if y is None:
             y = torch.empty((T, d), dtype=torch.float32 if y_dtype == F32 else torch.bfloat16, device=r.device)
-        assert y.shape == r.shape and types.get(y.dtype) == y_dtype
+        _want(y.shape == r.shape and types.get(y.dtype) == y_dtype, "y: [T, d] of y_dtype (BF16 or F32) is wanted")
         r_out = r if in_place else torch.empty_like(r)
         n_out = None if not pre_norm else n if in_place else torch.empty_like(n)
         kind = GATE_NONE if gate is None else GATE_TOKEN if per_token else GATE_CHANNEL
@@ -456,13 +466,13 @@ class DynamoLayer:
     def set_channel_precision(self, hi_bits):
         """Precision the significant channels of each routed expert are served at: int [E], each in {2,3,4,6,8}."""
         hb = np.ascontiguousarray(np.asarray(hi_bits, dtype=np.int32))
-        assert hb.shape == (self.desc.n_experts,)
+        _want(hb.shape == (self.desc.n_experts,), "hi_bits: [E] is wanted")
         _check(load().dynamo_set_channel_precision(self.ctx, _i32p(hb), _stream()), "dynamo_set_channel_precision")
 
     def set_channel_precision_down(self, hi_bits):
         """Precision the significant hidden units (d_ff side) of each routed expert are served at: int [E]."""
         hb = np.ascontiguousarray(np.asarray(hi_bits, dtype=np.int32))
-        assert hb.shape == (self.desc.n_experts,)
+        _want(hb.shape == (self.desc.n_experts,), "hi_bits: [E] is wanted")
         _check(load().dynamo_set_channel_precision_down(self.ctx, _i32p(hb), _stream()),
                "dynamo_set_channel_precision_down")
 
@@ -538,11 +548,11 @@ def assign_bits(x, levels, c: int = 4, m: float = 2.0, eps: float = 1e-9, max_it
     as_f64 = lambda a: None if a is None else np.ascontiguousarray(np.asarray(a, dtype=np.float64))
     u0a, sha = as_f64(u0), as_f64(token_share)
     if u0a is not None:
-        assert u0a.shape == (n, c)
+        _want(u0a.shape == (n, c), "u0: [n, c] is wanted")
     if sha is not None:
-        assert sha.shape == (n,)
+        _want(sha.shape == (n,), "token_share: [n] is wanted")
     lv = np.ascontiguousarray(np.asarray(levels, dtype=np.int32))
-    assert lv.shape == (c,)
+    _want(lv.shape == (c,), "levels: [c] is wanted")
     bits, cluster = np.zeros(n, np.int32), np.zeros(n, np.int32)
     V, U, iters = np.zeros((c, dim)), np.zeros((n, c)), np.zeros(1, np.int32)
     ptr = lambda a: None if a is None else a.ctypes.data_as(f64p)
