@@ -403,7 +403,8 @@ class DynamoLayer:
                       in_place: bool = False):
         """The layer and the join behind it: forward_router of n bf16 [T, d] (the normalised stream), its output normed, gated
         and added to the stream r [T, d], and the norm in front of the next block.  Returns (r_out, n_out), n_out None without
-        pre_norm; in_place: r and n themselves.  gate: [d], or fp32 [T, 1].  y: a buffer [T, d] of y_dtype for the layer's output."""
+        pre_norm; in_place: r and n themselves.  gate: [d], or fp32 [T, 1].  y: a buffer [T, d] of y_dtype for the layer's output.
+        Nothing is recorded for automatic differentiation: a tensor that requires its gradient is refused unless under torch.no_grad()."""
         T, d = r.shape
         types = {torch.bfloat16: BF16, torch.float32: F32}
         rows = [w for w in (w_post, w_pre) if w is not None]
@@ -411,6 +412,8 @@ class DynamoLayer:
         if gate is not None and not per_token:
             rows.append(gate)
         given = [r, n, w_router] + [t for t in (bias, w_post, gate, w_pre, y) if t is not None]
+        _want(not (torch.is_grad_enabled() and any(t.requires_grad for t in given)),
+              "a gradient is wanted, and this call records none (torch.no_grad())")
         device = r.device if self.workspace is None else self.workspace.device   # (no weights yet: the call itself refuses)
         _want(all(t.is_cuda and t.is_contiguous() and t.device == device for t in given), "contiguous tensors on the layer's CUDA device are wanted")
         _want(d == self.desc.d_model and r.dtype in types and n.shape == r.shape and n.dtype == torch.bfloat16, "r: [T, d] bfloat16 or float32, and n: [T, d] bfloat16 are wanted")

@@ -2,11 +2,12 @@
 // arithmetic is all behind the C-ABI (include/dynamo.h).  A small call is bound by what the host does for it: through ctypes, with
 // the same checks in Python, a combine of 64 tokens took 10.5 us and a gradient of the norm join 30, of which the launches are 3 and 5.
 //
-// A wrong tensor raises ValueError, what the library refuses DynamoError; torch's own errors pass through.
+// A wrong tensor raises ValueError (one that requires a gradient while gradients are recorded as well), what the library refuses DynamoError; torch's own errors pass through.
 #include <Python.h>
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -77,6 +78,9 @@ void on_cuda(const Tensor& t, const char* name) {
     if (!t.is_cuda() || t.layout() != at::kStrided) refuse(std::string(name) + ": a CUDA tensor is wanted");
 }
 void like(const Tensor& t, const char* name, c10::Device device) {
+    // (results without a graph would leave such a tensor without its gradient, and nobody would be told)
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        refuse(std::string(name) + ": its gradient is wanted, and this call records none (torch.no_grad() and the gradients' own calls)");
     if (t.layout() != at::kStrided || t.device() != device || !t.is_contiguous())
         refuse(std::string(name) + ": a contiguous tensor on " + device.str() + " is wanted");
 }

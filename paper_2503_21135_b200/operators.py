@@ -8,7 +8,8 @@ the stream are ``csrc/torch_binding.cpp``'s.
 Tensors are contiguous, on one CUDA device, 16-byte aligned; they may be on another device than the current one.  Work goes to
 the current stream of the tensors' device, and a tensor that another stream wrote or will free is the caller's to order, as with
 torch's own functions.  A wrong tensor raises ``ValueError`` before anything is launched, what the library refuses
-``binding.DynamoError``.  The functions do not take part in automatic differentiation: gradients are calls of their own.
+``binding.DynamoError``.  The functions do not take part in automatic differentiation: gradients are calls of their own, and a tensor
+that requires its gradient is refused (``ValueError``) unless torch records none (``torch.no_grad()``, ``detach()``).
 Results and scratch memory come from torch's allocator, so a call may be captured in a graph.
 """
 from __future__ import annotations
