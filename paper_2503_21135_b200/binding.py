@@ -422,6 +422,7 @@ class DynamoLayer:
         _want(all(w.shape == (d,) and w.dtype in types and w.dtype == rows[0].dtype for w in rows), "w_post, w_pre and a gate of the channels: [d], bfloat16 or float32, one type for all is wanted")
         _want(not per_token or (tuple(gate.shape) == (T, 1) and gate.dtype == torch.float32), "gate: [d] or float32 [T, 1] is wanted")
         _want((post_norm or w_post is None) and (pre_norm or w_pre is None), "w_post goes with post_norm, w_pre with pre_norm")
+        written = ([] if y is None else [y]) + ([r] + ([n] if pre_norm else []) if in_place else [])
         if y is None:
             y = torch.empty((T, d), dtype=torch.float32 if y_dtype == F32 else torch.bfloat16, device=r.device)
         _want(y.shape == r.shape and types.get(y.dtype) == y_dtype, "y: [T, d] of y_dtype (BF16 or F32) is wanted")
@@ -435,6 +436,9 @@ class DynamoLayer:
             st = load().dynamo_moe_block_forward(self.ctx, ctypes.byref(desc), ptr(r), ptr(n), ptr(w_router), ptr(bias), ptr(w_post),
                                                  ptr(gate), ptr(w_pre), T, ptr(y), ptr(r_out), ptr(n_out), None, None, _stream())
         _check(st, "dynamo_moe_block_forward")
+        for t in written:   # to automatic differentiation they are other tensors now (inference tensors count no versions)
+            if not t.is_inference():
+                torch.autograd.graph.increment_version(t)
         return r_out, n_out
 
     def forward_host(self, x_host: torch.Tensor, logits_host: torch.Tensor, y_host: torch.Tensor, y_dtype=F32):

@@ -116,6 +116,11 @@ struct OnDevice {
     void* stream;
     explicit OnDevice(c10::Device d) : guard(d), stream((void*)c10::cuda::getCurrentCUDAStream(d.index()).stream()) {}
 };
+// A tensor of the caller's has been written: to automatic differentiation it is another now.  (Inference tensors count no versions, and
+// nothing is kept of them.)
+void written(const Tensor& t) {
+    if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 PyObject* wrap(const Tensor& t) {
     if (t.defined()) return THPVariable_Wrap(t);
     Py_RETURN_NONE;
@@ -182,6 +187,8 @@ PyObject* dispatch(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check_status(dynamo_dispatch((const int32_t*)ptr(idx), T, E, k, ptr(x), d, code, (int32_t*)mut(offsets), (int32_t*)mut(perm),
                                  (int32_t*)mut(pos), mut(rows), mut(ws), need, on.stream),
                  "dynamo_dispatch");
+    if (!a.none(3))
+        for (const Tensor* t : {&rows, &offsets, &perm, &pos}) written(*t);
     return tuple_of(rows, offsets, perm, pos);
     END_HANDLE_TH_ERRORS
 }
@@ -227,6 +234,7 @@ PyObject* combine(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check_status(dynamo_combine(ptr(r.rows), r.code, (const int32_t*)ptr(r.pos), (const float*)ptr(r.w), r.T, r.k, r.d, mut(y),
                                 type_code(y, "out"), on.stream),
                  "dynamo_combine");
+    if (!a.none(4)) written(y);
     return wrap(y);
     END_HANDLE_TH_ERRORS
 }
@@ -253,6 +261,7 @@ PyObject* combine_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check_status(dynamo_combine_backward(ptr(dy), dy_code, ptr(r.rows), r.code, (const int32_t*)ptr(r.pos), (const float*)ptr(r.w),
                                          r.T, r.k, r.d, mut(d_rows), (float*)mut(d_w), on.stream),
                  "dynamo_combine_backward");
+    if (!a.none(4)) written(d_rows);
     return tuple_of(d_rows, d_w);
     END_HANDLE_TH_ERRORS
 }
@@ -347,6 +356,8 @@ PyObject* norm_join(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check_status(dynamo_norm_join_forward(&j.D, ptr(j.r), ptr(j.y), ptr(j.w_post), ptr(j.gate), ptr(j.w_pre), j.T, mut(r_out),
                                           mut(n_out), (float*)mut(stats), on.stream),
                  "dynamo_norm_join_forward");
+    if (!a.none(12)) written(r_out);
+    if (!a.none(13)) written(n_out);
     PyObject* res = PyTuple_New(want_stats ? 3 : 2);
     if (!res) throw python_error();
     if (j.y.defined() && a.none(12)) {
@@ -452,6 +463,7 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (need) ws = empty({(int64_t)need}, device, at::kByte);
     check_status(dynamo_linear_forward(ptr(x), T, N, K, G, ptr(codes), ptr(params), mut(y), type_code(y, "out"), mut(ws), need, on.stream),
                  "dynamo_linear_forward");
+    if (!a.none(4)) written(y);
     return wrap(y);
     END_HANDLE_TH_ERRORS
 }

@@ -1,8 +1,10 @@
-"""The operators around the layer are not differentiable by themselves: a tensor whose gradient is wanted is refused."""
+"""The operators around the layer are not differentiable by themselves: a tensor whose gradient is wanted is refused, and a tensor that a
+call writes counts as changed."""
 import pytest
 import torch
 
 from helpers import make_gpu_layer, make_inputs
+from paper_2503_21135_b200 import binding
 from paper_2503_21135_b200 import operators as ops
 from paper_2503_21135_b200 import workloads as wl
 
@@ -87,3 +89,44 @@ def test_block_forward(block):
     with torch.no_grad():
         got = gpu.forward_block(r, n, w_r, bias, w_post=p)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_written_tensors_count_as_changed():
+    idx, x, s = setup()
+    codes, params = ops.quantize_linear(x.bfloat16(), 64)
+    r, n = torch.zeros_like(x), torch.zeros((3, 64), dtype=torch.bfloat16, device="cuda")
+    y, out, d_rows = torch.zeros((3, 3), device="cuda"), torch.zeros_like(x), torch.zeros_like(s.rows)
+    for written, call in ((list(s), lambda: ops.dispatch(idx, 3, x, out=tuple(s))), ([out], lambda: ops.combine(s.rows, s.pos, out=out)),
+                          ([out], lambda: ops.dispatch_backward(s.rows, s.pos, out=out)),
+                          ([d_rows], lambda: ops.combine_backward(x, s.rows, s.pos, d_rows=d_rows)),
+                          ([r, n], lambda: ops.norm_join(r, x, r_out=r, n_out=n)),
+                          ([y], lambda: ops.linear(x.bfloat16(), codes, params, out=y))):
+        before = [t._version for t in written]
+        call()
+        assert [t._version for t in written] == [v + 1 for v in before]
+    # what autograd kept of a tensor that a call then wrote is not used for a gradient
+    leaf = torch.ones((3, 64), device="cuda", requires_grad=True)
+    loss = (leaf * out).sum()
+    ops.combine(s.rows, s.pos, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_inference_tensors_can_be_given():
+    """They have no version to count; torch keeps none of them for a gradient."""
+    idx, x, s = setup()
+    with torch.inference_mode():
+        out = torch.zeros((3, 64), device="cuda")
+    ops.combine(s.rows, s.pos, out=out)
+    assert torch.equal(out, ops.combine(s.rows, s.pos))
+
+
+def test_block_writes_count(block):
+    gpu, w_r, bias, r, n, w = block
+    r, n = r.clone(), n.clone()
+    y = torch.empty_like(r)
+    before = [t._version for t in (r, n, y)]
+    gpu.forward_block(r, n, w_r, bias, w_post=w, y=y, y_dtype=binding.BF16)
+    assert [t._version for t in (r, n, y)] == [before[0], before[1], before[2] + 1]
+    gpu.forward_block(r, n, w_r, bias, w_post=w, y=y, y_dtype=binding.BF16, in_place=True)
+    assert [t._version for t in (r, n, y)] == [before[0] + 1, before[1] + 1, before[2] + 2]
