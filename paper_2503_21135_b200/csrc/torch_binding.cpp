@@ -37,6 +37,18 @@ void check_status(dynamo_status st, const char* where) {
     throw python_error();
 }
 
+// A launch can wait (a stream takes about a thousand), and what it waits for may be another Python thread or a callback: the interpreter's
+// lock is given away for it, as torch's own calls do.  The arguments' tensors are held by the caller.
+struct Unlocked {
+    PyThreadState* const state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+template <typename F>
+dynamo_status unlocked(F f) {
+    const Unlocked u;
+    return f();
+}
+
 // Arguments arrive by position; None stands for what was left out.
 struct Args {
     PyObject* const* v;
@@ -184,9 +196,10 @@ PyObject* dispatch(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
     Tensor ws;
     if (need) ws = empty({(int64_t)need}, device, at::kByte);
-    check_status(dynamo_dispatch((const int32_t*)ptr(idx), T, E, k, ptr(x), d, code, (int32_t*)mut(offsets), (int32_t*)mut(perm),
-                                 (int32_t*)mut(pos), mut(rows), mut(ws), need, on.stream),
-                 "dynamo_dispatch");
+    check_status(unlocked([&] {
+        return dynamo_dispatch((const int32_t*)ptr(idx), T, E, k, ptr(x), d, code, (int32_t*)mut(offsets), (int32_t*)mut(perm),
+                               (int32_t*)mut(pos), mut(rows), mut(ws), need, on.stream);
+    }), "dynamo_dispatch");
     if (!a.none(3))
         for (const Tensor* t : {&rows, &offsets, &perm, &pos}) written(*t);
     return tuple_of(rows, offsets, perm, pos);
@@ -231,9 +244,11 @@ PyObject* combine(PyObject*, PyObject* const* args, Py_ssize_t n) {
         like(y, "out", r.device, y_type);
         shaped(y, "out", {r.T, r.d});
     }
-    check_status(dynamo_combine(ptr(r.rows), r.code, (const int32_t*)ptr(r.pos), (const float*)ptr(r.w), r.T, r.k, r.d, mut(y),
-                                type_code(y, "out"), on.stream),
-                 "dynamo_combine");
+    const int32_t y_code = type_code(y, "out");
+    check_status(unlocked([&] {
+        return dynamo_combine(ptr(r.rows), r.code, (const int32_t*)ptr(r.pos), (const float*)ptr(r.w), r.T, r.k, r.d, mut(y),
+                              y_code, on.stream);
+    }), "dynamo_combine");
     if (!a.none(4)) written(y);
     return wrap(y);
     END_HANDLE_TH_ERRORS
@@ -258,9 +273,10 @@ PyObject* combine_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
         shaped(d_rows, "d_rows", r.rows.sizes());
     }
     if (a.truth(5)) d_w = empty({r.T, r.k}, r.device, at::kFloat);
-    check_status(dynamo_combine_backward(ptr(dy), dy_code, ptr(r.rows), r.code, (const int32_t*)ptr(r.pos), (const float*)ptr(r.w),
-                                         r.T, r.k, r.d, mut(d_rows), (float*)mut(d_w), on.stream),
-                 "dynamo_combine_backward");
+    check_status(unlocked([&] {
+        return dynamo_combine_backward(ptr(dy), dy_code, ptr(r.rows), r.code, (const int32_t*)ptr(r.pos), (const float*)ptr(r.w),
+                                       r.T, r.k, r.d, mut(d_rows), (float*)mut(d_w), on.stream);
+    }), "dynamo_combine_backward");
     if (!a.none(4)) written(d_rows);
     return tuple_of(d_rows, d_w);
     END_HANDLE_TH_ERRORS
@@ -353,9 +369,10 @@ PyObject* norm_join(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
     const bool want_stats = a.truth(11);
     if (want_stats) stats = empty({j.T, 2}, j.device, at::kFloat);
-    check_status(dynamo_norm_join_forward(&j.D, ptr(j.r), ptr(j.y), ptr(j.w_post), ptr(j.gate), ptr(j.w_pre), j.T, mut(r_out),
-                                          mut(n_out), (float*)mut(stats), on.stream),
-                 "dynamo_norm_join_forward");
+    check_status(unlocked([&] {
+        return dynamo_norm_join_forward(&j.D, ptr(j.r), ptr(j.y), ptr(j.w_post), ptr(j.gate), ptr(j.w_pre), j.T, mut(r_out),
+                                        mut(n_out), (float*)mut(stats), on.stream);
+    }), "dynamo_norm_join_forward");
     if (!a.none(12)) written(r_out);
     if (!a.none(13)) written(n_out);
     PyObject* res = PyTuple_New(want_stats ? 3 : 2);
@@ -406,10 +423,11 @@ PyObject* norm_join_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check_status(dynamo_norm_join_workspace_bytes(&j.D, j.T, &need), "dynamo_norm_join_workspace_bytes");
     if (d_w_post.defined() || d_w_pre.defined() || j.D.gate_kind == DYNAMO_GATE_CHANNEL) ws = empty({(int64_t)need}, j.device, at::kByte);
     else need = 0;
-    check_status(dynamo_norm_join_backward(&j.D, ptr(d_n), ptr(d_ro), ptr(j.r), ptr(j.y), (const float*)ptr(stats), ptr(j.w_post),
-                                           ptr(j.gate), ptr(j.w_pre), j.T, mut(d_r), mut(d_y), (float*)mut(d_w_post),
-                                           (float*)mut(d_gate), (float*)mut(d_w_pre), mut(ws), need, on.stream),
-                 "dynamo_norm_join_backward");
+    check_status(unlocked([&] {
+        return dynamo_norm_join_backward(&j.D, ptr(d_n), ptr(d_ro), ptr(j.r), ptr(j.y), (const float*)ptr(stats), ptr(j.w_post),
+                                         ptr(j.gate), ptr(j.w_pre), j.T, mut(d_r), mut(d_y), (float*)mut(d_w_post),
+                                         (float*)mut(d_gate), (float*)mut(d_w_pre), mut(ws), need, on.stream);
+    }), "dynamo_norm_join_backward");
     return tuple_of(d_r, d_y, d_w_post, d_gate, d_w_pre);
     END_HANDLE_TH_ERRORS
 }
@@ -427,7 +445,9 @@ PyObject* quantize_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int32_t N = size32(w.size(0), "w"), K = size32(w.size(1), "w");
     const OnDevice on(w.device());
     Tensor codes = empty({N, K / 2}, w.device(), at::kByte), params = empty({N, K / G, 2}, w.device(), at::kHalf);
-    check_status(dynamo_linear_quantize(ptr(w), N, K, (int32_t)G, mut(codes), mut(params), on.stream), "dynamo_linear_quantize");
+    check_status(unlocked([&] {
+        return dynamo_linear_quantize(ptr(w), N, K, (int32_t)G, mut(codes), mut(params), on.stream);
+    }), "dynamo_linear_quantize");
     return tuple_of(codes, params);
     END_HANDLE_TH_ERRORS
 }
@@ -461,8 +481,10 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     check_status(dynamo_linear_workspace_bytes(T, N, K, G, &need), "dynamo_linear_workspace_bytes");
     Tensor ws;
     if (need) ws = empty({(int64_t)need}, device, at::kByte);
-    check_status(dynamo_linear_forward(ptr(x), T, N, K, G, ptr(codes), ptr(params), mut(y), type_code(y, "out"), mut(ws), need, on.stream),
-                 "dynamo_linear_forward");
+    const int32_t y_code = type_code(y, "out");
+    check_status(unlocked([&] {
+        return dynamo_linear_forward(ptr(x), T, N, K, G, ptr(codes), ptr(params), mut(y), y_code, mut(ws), need, on.stream);
+    }), "dynamo_linear_forward");
     if (!a.none(4)) written(y);
     return wrap(y);
     END_HANDLE_TH_ERRORS

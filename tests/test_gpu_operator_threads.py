@@ -1,11 +1,13 @@
 """The operators around the layer called by several host threads at a time."""
 import ctypes
 import threading
+import time
 
 import pytest
 import torch
 
 from paper_2503_21135_b200 import binding
+from paper_2503_21135_b200 import operators as ops
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +45,40 @@ def test_wide_gradients_side_by_side():
     for t in threads:
         t.join()
     assert not failed
+
+
+@pytest.mark.parametrize("name", ["dispatch", "combine", "combine_backward", "norm_join", "norm_join_backward", "quantize_linear", "linear"])
+def test_other_threads_run_while_a_launch_waits(name):
+    """Launches behind a kernel of about a second, more than a stream takes: the caller waits in a launch, another thread goes on."""
+    idx, x = torch.zeros((8, 1), dtype=torch.int32, device="cuda"), torch.ones((8, 256), dtype=torch.bfloat16, device="cuda")
+    s = ops.dispatch(idx, 1, x)
+    stats = ops.norm_join(x, want_stats=True)[2]
+    codes, params = ops.quantize_linear(x)
+    n_out, y = torch.empty_like(x), torch.empty((8, 8), device="cuda")
+    d_rows = torch.empty_like(s.rows)
+    call = {"dispatch": lambda: ops.dispatch(idx, 1, x, out=tuple(s)), "combine": lambda: ops.combine(s.rows, s.pos, out=n_out),
+            "combine_backward": lambda: ops.combine_backward(x, s.rows, s.pos, d_rows=d_rows, want_d_w=False),
+            "norm_join": lambda: ops.norm_join(x, n_out=n_out), "norm_join_backward": lambda: ops.norm_join_backward(x, None, x, None, stats),
+            "quantize_linear": lambda: ops.quantize_linear(x), "linear": lambda: ops.linear(x, codes, params, out=y)}[name]
+    torch.cuda.synchronize()
+    gaps, stop = [0.0], threading.Event()
+
+    def watch():
+        last = time.perf_counter()
+        while not stop.is_set():
+            time.sleep(0.001)
+            now = time.perf_counter()
+            gaps[0], last = max(gaps[0], now - last), now
+
+    watcher = threading.Thread(target=watch)
+    watcher.start()
+    t0 = time.perf_counter()
+    torch.cuda._sleep(2_000_000_000)
+    for _ in range(6000):
+        call()
+    waited = time.perf_counter() - t0
+    stop.set()
+    watcher.join()
+    torch.cuda.synchronize()
+    assert waited > 0.5, "the queue was not full: nothing was tested"
+    assert gaps[0] < 0.3
