@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const 
 // the pairs) and its tokens' rows copied, one read and k writes each, 16 bytes a thread and four of them at a time.
 // Every CTA counts the whole array, so one of 1024 threads an SM: 4096 tokens of 8 KB, top-2 of 8 experts, 21.8 us (4.6 TB/s;
 // some 4 us of it in front of the first copy), 24.2 with four CTAs of 256.  Asking for the rows ahead of the count (into the
-// L2, 64 to 256 KB a CTA) made it 22.5, eight pieces a thread at a time 22.2: it is the writes that bound it.
+// L2, 64 to 256 KB a CTA) made it 22.5, eight pieces a thread at a time 22.2.
 __global__ void __launch_bounds__(DISPATCH_THREADS, 1) dispatch_kernel(const __grid_constant__ DispatchArgs a) {
     __shared__ int s_total[DISPATCH_EXPERTS], s_next[DISPATCH_EXPERTS];
     __shared__ int s_hist[DISPATCH_WARPS][DISPATCH_EXPERTS];

@@ -863,10 +863,10 @@ static cudaError_t linear_few(LinearArgs a, int y_f32, int n_sms, cudaStream_t s
 // nothing to set up; the tcgen05 kernel has two launches beside it and the start of its pipeline, about 10 us, and then takes
 // twice the codes in the same time.  So the rule is on the weights times the tiles of 16 (us, few-token against tcgen05):
 //   2^20 2.9 / 10.1,  2^24 6.4 / 12.1 (64 tokens, 2048 x 2048),  2^25 10.6 / 15.8 (64, 2048 x 4096) and 10.9 / 14.8 (32, 4096 x 4096),
-//   56 * 2^20 20.0 / 19.3 (16, 14336 x 4096),  2^26 18.8 / 18.9 (16, 8192 x 8192) and 21.1 / 19.0 (64, 4096 x 4096),
-//   2^27 35.9 / 20.3 (128, 4096 x 4096),  196 * 2^20 57.4 / 39.3 (16, 14336 x 14336).
-// With 8 tokens the few-token kernel has one MMA a step and keeps up with the codes: 41.3 us at 14336 x 14336, the other 39.0 us.
-// (The tcgen05 kernel's figures are from before its operand was freed of the 16: 2 to 5% more now, 42.2 in the last of the table.)
+//   56 * 2^20 20.0 / 20.1 (16, 14336 x 4096),  2^26 18.8 / 20.8 (16, 8192 x 8192) and 21.1 / 17.0 (64, 4096 x 4096),
+//   2^27 35.9 / 20.5 (128, 4096 x 4096),  196 * 2^20 57.4 / 42.2 (16, 14336 x 14336).
+// (Up to 2^25 the tcgen05 kernel's figures are from before its operand was freed of the 16: 2 to 5% more now.)  Up to 8 tokens the few-token
+// kernel has half of the MMAs: 41.4 us at 14336 x 14336, 40% of the copy rate, and the tcgen05 kernel is no faster there.
 static int tc_tile(int T, int rows, int cols) {
     if (T <= 8 || (T + 15) / 16 * (long long)rows * cols <= 3ll << 24) return 0;
     return T <= 16 ? 16 : T <= 32 ? 32 : 64;

@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(threads_of(TPR), ctas_of(threads_of(TPR), join
 
 // The gradient, laid out the same.  What the first pass over a row has worked out in fp32 (r', dr' + s_r u, y, dn) stays in
 // registers for the second; the next row's loads go out once it has read the present one's registers.  4096 rows of 4096, bf16,
-// gate per channel: 42.9 us with the launch that adds up the CTAs' sums (4.7 TB/s); 47 with every sum reduced by itself and a
+// gate per channel: 43.4 us with the launch that adds up the CTAs' sums (4.7 TB/s); 47 with every sum reduced by itself and a
 // copy of the row that came, 56 with the rows staged in shared memory and read twice.  The column sums of d_w_post and of a channel gate differ by a factor of the column
 // (S1 = sum_t block_scale gate_t G y s_y; d_w_post = gate S1, d_gate = w_post S1), so that two sums a column are kept.
 template <typename TY, typename TR, typename TN, int TPR, int V, bool KEEP>

@@ -10,7 +10,8 @@ the current stream of the tensors' device, and a tensor that another stream wrot
 torch's own functions.  A wrong tensor raises ``ValueError`` before anything is launched, what the library refuses
 ``binding.DynamoError``.  The functions do not take part in automatic differentiation: gradients are calls of their own, and a tensor
 that requires its gradient is refused (``ValueError``) unless torch records none (``torch.no_grad()``, ``detach()``).
-Results and scratch memory come from torch's allocator, so a call may be captured in a graph.
+Results and scratch memory come from torch's allocator, so a call may be captured in a graph.  A tensor that is given for a result (out,
+d_rows, r_out, n_out) overlaps no input and no other result, but r_out may be r.
 """
 from __future__ import annotations
 
