@@ -356,6 +356,13 @@ __device__ __forceinline__ uint32_t bar_test(uint32_t bar, uint32_t parity) {
     return ok;
 }
 
+// Behind a thread's own reads of a place in shared memory and in front of the arrival that gives the place back to be filled by a
+// bulk copy.  The copy writes through the async proxy: only this fence orders reads in front of it.  Without it a read that an
+// SM's busy memory pipeline holds up is overtaken: the arrival does not wait for it (4-bit product of 16 tokens with cold caches:
+// every third launch had wrong results in a few tiles).  Not needed where the arrival is behind an instruction that cannot be
+// issued without the values read, a store to tensor memory for instance.
+__device__ __forceinline__ void reads_done() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // 1-D bulk async copy global -> shared, completion counted on an mbarrier (bytes % 16 == 0,
 // both addresses 16-byte aligned).
 __device__ __forceinline__ void bulk_g2s(void* smem_dst, const void* gsrc, uint32_t bytes, uint64_t* bar) {
