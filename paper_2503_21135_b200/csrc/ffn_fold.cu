@@ -377,6 +377,7 @@ __device__ __forceinline__ bool ff_fold_item(const FfParams& p, const FfItem& im
                     tc_ld_rows16(acc + c0 + 16, r[(c0 / 16 + 1) & 1]);
                 } else {   // the buffer is read: hand it back to the MMA warp, and the stage to the producer
                     tc_fence_before();
+                    if (g == NG - 1) reads_done();
                     __syncwarp();
                     if (lane == 0) {
                         bar_arrive(FF_BAR(acc_empty, acb.i));

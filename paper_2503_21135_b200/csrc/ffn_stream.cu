@@ -252,6 +252,7 @@ __device__ __forceinline__ bool consume_item(const FfnParams& p, FfnSmem* S, uin
                 }
             }
         }
+        reads_done();
         __syncwarp();
         if (lane == 0) mbar_arrive(&S->empty[s]);
     }
@@ -285,6 +286,7 @@ __device__ __forceinline__ bool consume_item(const FfnParams& p, FfnSmem* S, uin
                     for (int j = 0; j < NT8; ++j) mma16816(total[a][j], af, b0[j], b1[j]);
                 }
             }
+            reads_done();
             __syncwarp();
             if (lane == 0) mbar_arrive(&S->empty[s]);
         }

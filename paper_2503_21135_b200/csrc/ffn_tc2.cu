@@ -256,6 +256,7 @@ __device__ __forceinline__ int t2_dequant_run(const T2Deq& c, int n, uint32_t gi
         tc_st_x4(c.a_lanes + 64 * b, regs);
         t2_dequant_half<BITS, 1>(raw, prm[0][NG - 1], prm[1][NG - 1], regs);
         // the codes are used: their place in the ring can go back to the producer
+        reads_done();
         __syncwarp();
         if (c.lane == 0) bar_arrive(T2_BAR(empty, gi % T2_NW));
         const uint32_t xready = bar_test(T2_BAR(fullx, b), (gi / T2_NX) & 1);

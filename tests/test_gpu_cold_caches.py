@@ -3,7 +3,9 @@ kernel run far apart; a place in shared memory that is filled again too early, o
 import pytest
 import torch
 
+from helpers import make_gpu_layer, make_inputs
 from paper_2503_21135_b200 import operators as ops
+from paper_2503_21135_b200 import workloads as wl
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +37,24 @@ def test_linear(T, N, K, G):
     x = torch.randn((T, K), generator=g, device="cuda").bfloat16()
     assert repeated(lambda: ops.linear(x, codes, params), 300) == 0
     assert ops.poll_linear_status() == 0
+
+
+@pytest.fixture(scope="module", params=[("tiny", dict(d_model=2048, d_ff=4096)), ("finegrained", dict(n_experts=16, n_shared=1))],
+                ids=["G128", "G64"])
+def layer(request):
+    name, kw = request.param
+    cfg = wl.scaled(wl.CONFIGS[name], **kw)
+    wg, wu, wd, bits, pool, sets = make_inputs(cfg)
+    gpu = make_gpu_layer(cfg, wg, wu, wd, bits, pool, max_tokens=1024)
+    gpu.set_channel_switch(sets)
+    return cfg, gpu
+
+
+@pytest.mark.parametrize("T", [1, 8, 40, 139, 500, 1000])   # streaming, fold and pair kernels
+def test_layer(layer, T):
+    cfg, gpu = layer
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn((T, cfg.d_model), generator=g, device="cuda").bfloat16()
+    logits = torch.randn((T, cfg.n_experts), generator=g, device="cuda")
+    assert repeated(lambda: gpu.forward(x, logits), 300) == 0
+    assert gpu.poll_status() == 0
