@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 //                  row's codes; a row a lane kept the L1 busy with 32 lines a load).  The codes come by cp.async, three jobs of a warp
 //                  on their way: 96 KB an SM (one job in registers left the loads' latency to bind)
 //   8-    fold   : (lane quarter, row tile) each, a row a lane; per group  y += s * acc + m * sum(x); sixteen warps at 64
-//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 82.4 / 57.5 us; as 78.3 / 55.4 they were compared, before the
+//                  tokens, half of the columns each (14336 x 14336, 64 tokens, groups of 64 / 128: 82 / 58 us; as 78.3 / 55.4 they were compared, before the
 //                  operand's 16 went off in the expansion, with packed pairs, whose moves and registers cost more than the instructions
 //                  they save, 85.1 / 54.1, and both halves of the columns on their way
 //                  90.0 / 53.7, spilling; eight warps 107 / 50.6; sixteen of a quarter of the columns and both row tiles, half the reads of
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(32 * LIN_WARPS) linear_few_kernel(const __grid
 // Roles meet at barriers only, so that the chain of a stage (codes, expansion, MMAs, fold) overlaps its neighbours', blocks' ends
 // included; the same work by eight warps that all did every part, a barrier of the CTA a stage, took 88 us at 64 tokens, 14336 x 14336.
 // Bound by the fold at 64 tokens (63% of the issue slots at groups of 64), by the expansion and the hand-overs at 32 and fewer:
-// 45.7 us at 14336 x 14336 and 32 tokens, 2.4 TB/s of codes and parameters.  The subtraction that makes 16 + q a q is 2 to 5% of the time.
+// 46 us at 14336 x 14336 and 32 tokens, 2.4 TB/s of codes and parameters.  The subtraction that makes 16 + q a q is 2 to 5% of the time.
 // A block that lies within one CTA's run goes from the fold warps' registers to y; the pieces of the others go to the workspace, and a
 // kernel behind this one adds them up in the order of the CTAs.
 // Tensor memory: two A buffers of 128 columns, then BUFS accumulator buffers of 2 * TOK, one a group.
